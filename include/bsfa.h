@@ -224,6 +224,98 @@ bsfa_status bsfa_calibrate_topk(const bsfa_problem *p, const void *q, const void
  * invalid). */
 size_t bsfa_calibrate_workspace_bytes(const bsfa_problem *p);
 
+/* ---- paged K/V cache ------------------------------------------------------------------------------
+ *
+ * What serving needs around bsfa_forward: new tokens' keys and values are appended to a cache that is kept in
+ * pages of page_size tokens (rotated by their positions on the way), and later tokens attend to it.  Token t of a
+ * batch element lies in page block_table[t / page_size] of the element's row, at place t % page_size.  Page ids
+ * outside [0, n_pages) hold nothing: appending drops what would go there, attention does not see it.
+ * The three entry points enqueue kernels only: no allocation, no copy, no host synchronisation.  They may be
+ * captured into a graph; lengths, positions and tables are read when the graph runs. */
+typedef struct {
+    int32_t n_pages, page_size;   /* page_size: a power of two, at least 16 */
+    int32_t n_kv_heads, head_dim; /* head_dim 64 or 128 */
+    int32_t dtype;                /* bsfa_dtype of the cache and of every q, k, v and out used with it */
+    int64_t k_stride_page, k_stride_n, k_stride_h;   /* element strides: page, token in it, head.  Pages of [token, */
+    int64_t v_stride_page, v_stride_n, v_stride_h;   /* head, d] and of [head, token, d] are both expressible.      */
+    void *k, *v;                  /* DEVICE */
+} bsfa_cache;
+
+/* Zero-initialise it: a zero in an optional member selects its default. */
+typedef struct {
+    int32_t batch, n_q_heads, seqlen;   /* seqlen: rows of q, k and v for each batch element */
+    int64_t q_stride_b, q_stride_n, q_stride_h, k_stride_b, k_stride_n, k_stride_h, v_stride_b, v_stride_n, v_stride_h;
+    int64_t qo_stride_b, qo_stride_n, qo_stride_h, ko_stride_b, ko_stride_n, ko_stride_h;   /* q_out, k_out */
+    const int32_t *seqlens;       /* optional, DEVICE [batch]: new tokens of each element, clamped to [0, seqlen]; rows
+                                     behind them are neither read nor written.  NULL: all have seqlen. */
+    const int32_t *start;         /* DEVICE [batch]: position of each element's first new token (the tokens it has in
+                                     the cache already).  Tokens whose position lies outside the block table are left
+                                     out altogether: nothing is written for them. */
+    const int32_t *block_table;   /* DEVICE [batch] rows of table_pages page ids */
+    int64_t table_stride_b;
+    int32_t table_pages;
+    const float *cos_sin;         /* optional, DEVICE [n_positions][rot_dim], contiguous, 16-byte aligned: of every
+                                     position the cosines of its rot_dim / 2 angles, then their sines.  NULL: nothing
+                                     is rotated (q must be NULL then). */
+    int32_t n_positions;          /* at least table_pages * page_size: every position the table can hold */
+    int32_t rot_dim;              /* rotated elements of a head: a multiple of 16, at most head_dim; the others pass */
+    int32_t interleaved;          /* 0: element i is turned with i + rot_dim / 2; 1: 2 i with 2 i + 1 */
+} bsfa_append;
+
+/*
+ * Rotates the new tokens' keys by their positions, writes keys and values into the cache, and writes the rotated
+ * queries to q_out and, if k_out is not NULL, the rotated keys there as well (what bsfa_forward takes for a prompt):
+ *   (a, b) -> (a cos - b sin, b cos + a sin) for every pair, in 32 bits, rounded once.
+ * q_out may be q and k_out may be k.  q NULL: keys and values only.  No two tokens of a call may have the same place.
+ */
+bsfa_status bsfa_cache_append(const bsfa_cache *c, const bsfa_append *p, const void *q, const void *k, const void *v,
+                              void *q_out, void *k_out, void *hip_stream);
+
+/* Zero-initialise it: a zero in an optional member selects its default. */
+typedef struct {
+    int32_t batch, n_q_heads, seqlen;   /* seqlen: new tokens (rows of q) of each batch element, one or more */
+    int64_t q_stride_b, q_stride_n, q_stride_h, o_stride_b, o_stride_n, o_stride_h;
+    const int32_t *q_lens;        /* optional, DEVICE [batch]: new tokens of each element, clamped to [0, seqlen]; rows of
+                                     out and lse behind them are left untouched.  NULL: all have seqlen. */
+    const int32_t *cache_lens;    /* DEVICE [batch]: tokens each element has in its own pages, the new ones included,
+                                     clamped to what the block table holds.  May be 0. */
+    const int32_t *block_table;   /* DEVICE [batch] rows of table_pages page ids */
+    int64_t table_stride_b;
+    int32_t table_pages;
+    int32_t max_cache_len;        /* optional bound that cache_lens are clamped to as well; 0: what the table holds.  It
+                                     lets the host see that all sequences are short, and saves a kernel then. */
+    const int32_t *prefix_table;  /* bsfa_prefix_attention only, DEVICE: page ids of the shared prefix */
+    int32_t prefix_len;           /* ... its tokens: they lie before every element's own */
+    int32_t prefix_pages;         /* ... length of prefix_table, which must hold them */
+    void   *workspace;            /* DEVICE, 256-byte aligned: scratch memory of the call (calls that overlap need one
+                                     each), overwritten */
+    int64_t workspace_bytes;      /* at least bsfa_paged_workspace_bytes() */
+} bsfa_paged;
+
+/*
+ * Attention of each element's last q_lens[b] tokens over its cache_lens[b] tokens:
+ *   out_i = sum_t softmax_t(q_i k_t / sqrt(d)) v_t
+ * causal != 0: new token i, at place cache_lens[b] - q_lens[b] + i, sees the places up to its own; causal == 0: all.
+ * A row that sees nothing becomes 0, its lse -INFINITY.  lse (may be NULL): fp32 [batch][seqlen][n_q_heads], natural
+ * units.  Query head h reads KV head h / (n_q_heads / n_kv_heads).  Scores, softmax and accumulators are fp32, the
+ * probabilities are rounded to the element type for the second product.  Keys and values of places that some row of the
+ * element sees must be finite; what else lies in the pages has no influence, NaN included.
+ */
+bsfa_status bsfa_paged_attention(const bsfa_cache *c, const bsfa_paged *p, const void *q, int causal, void *out, float *lse,
+                                 void *hip_stream);
+
+/*
+ * The same where all elements share the prefix_len tokens of prefix_table's pages, which every new token sees before its
+ * element's own (cache_lens and block_table count those alone).  The prefix is read once for the whole batch, not once for
+ * each element.
+ */
+bsfa_status bsfa_prefix_attention(const bsfa_cache *c, const bsfa_paged *p, const void *q, int causal, void *out, float *lse,
+                                  void *hip_stream);
+
+/* Bytes of workspace the two need for *p; 0 where they use none, and if *p is invalid.  With prefix_table NULL for
+ * bsfa_paged_attention, else for bsfa_prefix_attention. */
+size_t bsfa_paged_workspace_bytes(const bsfa_cache *c, const bsfa_paged *p);
+
 /* Tile shapes and head dims this build supports: fills up to `cap` entries of each array with
  * (block_m, block_n, head_dim) triples and returns the number of supported triples. */
 int bsfa_query_build(int32_t *block_m, int32_t *block_n, int32_t *head_dim, int cap);

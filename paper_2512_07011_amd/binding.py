@@ -19,7 +19,8 @@ STATUS_NAMES = {0: "BSFA_OK", -1: "BSFA_ERR_NULL", -2: "BSFA_ERR_SHAPE", -3: "BS
                 -4: "BSFA_ERR_UNSUPPORTED", -5: "BSFA_ERR_WORKSPACE", -6: "BSFA_ERR_HIP"}
 EXPORTS = ["bsfa_forward", "bsfa_forward_workspace_bytes", "bsfa_calibrate", "bsfa_calibrate_noalloc",
            "bsfa_calibrate_noalloc_max_values", "bsfa_calibrate_topk",
-           "bsfa_calibrate_workspace_bytes", "bsfa_query_build",
+           "bsfa_calibrate_workspace_bytes", "bsfa_query_build", "bsfa_cache_append", "bsfa_paged_attention",
+           "bsfa_prefix_attention", "bsfa_paged_workspace_bytes",
            "bsfa_mfma_rate_probe", "bsfa_mfma_rate_probe_sink_bytes", "bsfa_mfma_rate_probe_flops",
            "bsfa_status_string", "bsfa_last_error"]
 
@@ -53,6 +54,29 @@ class bsfa_problem(ctypes.Structure):
 class bsfa_skip_stats(ctypes.Structure):
     _fields_ = [("counts", ctypes.c_void_p), ("skip_mask", ctypes.c_void_p), ("block_max", ctypes.c_void_p),
                 ("lse", ctypes.c_void_p)]
+
+
+class bsfa_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")] + \
+               [(n, ctypes.c_int64) for n in ("k_stride_page", "k_stride_n", "k_stride_h", "v_stride_page", "v_stride_n", "v_stride_h")] + \
+               [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
+class bsfa_append(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "seqlen")] + \
+               [("%s_stride_%s" % (t, x), ctypes.c_int64) for t in ("q", "k", "v", "qo", "ko") for x in "bnh"] + \
+               [("seqlens", ctypes.c_void_p), ("start", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("table_stride_b", ctypes.c_int64), ("table_pages", ctypes.c_int32), ("cos_sin", ctypes.c_void_p),
+                ("n_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class bsfa_paged(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "seqlen")] + \
+               [("%s_stride_%s" % (t, x), ctypes.c_int64) for t in "qo" for x in "bnh"] + \
+               [("q_lens", ctypes.c_void_p), ("cache_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("table_stride_b", ctypes.c_int64), ("table_pages", ctypes.c_int32), ("max_cache_len", ctypes.c_int32),
+                ("prefix_table", ctypes.c_void_p), ("prefix_len", ctypes.c_int32), ("prefix_pages", ctypes.c_int32),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
 
 
 _lib = None
@@ -97,6 +121,13 @@ def lib() -> ctypes.CDLL:
         L.bsfa_mfma_rate_probe_sink_bytes.argtypes = [ctypes.c_int]
         L.bsfa_mfma_rate_probe_flops.restype = ctypes.c_double
         L.bsfa_mfma_rate_probe_flops.argtypes = [ctypes.c_int, ctypes.c_int]
+        L.bsfa_cache_append.restype = ctypes.c_int
+        L.bsfa_cache_append.argtypes = [ctypes.POINTER(bsfa_cache), ctypes.POINTER(bsfa_append), vp, vp, vp, vp, vp, vp]
+        for f in (L.bsfa_paged_attention, L.bsfa_prefix_attention):
+            f.restype = ctypes.c_int
+            f.argtypes = [ctypes.POINTER(bsfa_cache), ctypes.POINTER(bsfa_paged), vp, ctypes.c_int, vp, vp, vp]
+        L.bsfa_paged_workspace_bytes.restype = ctypes.c_size_t
+        L.bsfa_paged_workspace_bytes.argtypes = [ctypes.POINTER(bsfa_cache), ctypes.POINTER(bsfa_paged)]
         L.bsfa_status_string.restype = ctypes.c_char_p
         L.bsfa_status_string.argtypes = [ctypes.c_int]
         L.bsfa_last_error.restype = ctypes.c_char_p
@@ -328,6 +359,194 @@ def bsfa_calibrate_topk(samples, ks: Sequence[int], causal: bool = True, block_m
         done += q.shape[0]
     q0 = samples[0][0]
     return torch.frombuffer(out, dtype=torch.float32).clone().view(n, q0.shape[2], n_tiles(q0.shape[1], block_m))
+
+
+# ---- paged K/V cache ---------------------------------------------------------------------------------------
+def alloc_cache(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda"):
+    """Keys and values of a paged cache, [n_pages, page_size, n_kv_heads, head_dim] each; a head's tokens lie together in
+    a page.  (The entry points take any other order with a contiguous last dimension as well.)"""
+    return tuple(torch.empty(n_pages, n_kv_heads, page_size, head_dim, dtype=dtype, device=device).transpose(1, 2) for _ in "kv")
+
+
+def rotary_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """[n_positions, rot_dim] fp32: of every position the cosines of its rot_dim / 2 angles
+    position * base ** (-2 i / rot_dim), then their sines.  The angles are taken in 64 bits."""
+    freq = base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device) / rot_dim)
+    angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * freq
+    return torch.cat([angle.cos(), angle.sin()], dim=1).float()
+
+
+def _same_device(name, q, *ts):
+    d = q.device
+    if d.type != "cuda":
+        raise ValueError("bsfa: tensors must live on the GPU")
+    for t in ts:
+        if t is not None and t.device != d:
+            raise ValueError("%s: tensors must live on one GPU" % name)
+
+
+def _on_device(device, call, *args):
+    """call(*args) with `device` current: the kernels of a stream are launched from its own device."""
+    if device.index == torch.cuda.current_device():
+        rc = call(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args)
+    if rc != BSFA_OK:
+        _check(rc)
+
+
+def _ints(name, t, *shape):
+    """Address of an int32 tensor of the given shape (None: any size), contiguous in its last dimension."""
+    if t.dtype != torch.int32 or t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise TypeError("%s must be int32 of shape %s, contiguous in its last dimension" % (name, list(shape)))
+    return t.data_ptr()
+
+
+def _rows(name, t, *shape):
+    """Strides of a [B, N, H, d] tensor (batch, token, head)."""
+    if t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, list(t.shape), list(shape)))
+    st = t.stride()
+    if st[3] != 1:
+        raise ValueError("%s: head dimension must be contiguous" % name)
+    return st[:3]
+
+
+def _cache(name, k_cache, v_cache):
+    if k_cache.dim() != 4 or k_cache.dtype not in DTYPES:
+        raise TypeError("%s: k_cache must be [n_pages, page_size, n_kv_heads, head_dim], bfloat16 or float16" % name)
+    shape = k_cache.shape
+    return bsfa_cache(*shape, DTYPES[k_cache.dtype], *_rows("k_cache", k_cache, *shape), *_rows("v_cache", v_cache, *shape),
+                      k_cache.data_ptr(), v_cache.data_ptr())
+
+
+def bsfa_cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                      block_table: torch.Tensor, start: torch.Tensor, cos_sin: Optional[torch.Tensor] = None,
+                      seqlens: Optional[torch.Tensor] = None, interleaved: bool = False, q_out: Optional[torch.Tensor] = None,
+                      k_out=None, stream: Optional[torch.cuda.Stream] = None):
+    """Appends the new tokens k, v [B,N,Hkv,d] to the paged cache [n_pages, page_size, Hkv, d]: element b's token i goes to
+    position start[b] + i, that is to page block_table[b, position // page_size].  ``cos_sin`` (fp32 [positions, rot_dim],
+    see rotary_table; at least as many positions as a row of the table holds) rotates keys and queries by their positions;
+    without it q must be None.  ``seqlens`` (int32 GPU tensor [B]) gives each element its own number of new tokens: rows
+    behind it are left alone.  ``interleaved``: adjacent elements are a pair, not halves.
+    Returns the rotated queries (``q_out``, which may be q; None without q) and, where ``k_out`` is True or a tensor, the
+    rotated keys: what bsfa_forward takes for a prompt; else None.  Enqueues on ``stream`` (default: torch's current
+    stream)."""
+    name = "bsfa_cache_append"
+    kt = k_out if isinstance(k_out, torch.Tensor) else None
+    _same_device(name, k, q, v, k_cache, v_cache, block_table, start, cos_sin, seqlens, q_out, kt)
+    c = _cache(name, k_cache, v_cache)
+    if k.dim() != 4 or (q is not None and q.dim() != 4):
+        raise ValueError("%s: q, k and v must be [B, N, H, d]" % name)
+    if k.shape[2:] != k_cache.shape[2:]:
+        raise ValueError("%s: k has heads %s, the cache %s" % (name, list(k.shape[2:]), list(k_cache.shape[2:])))
+    if any(t is not None and t.dtype != k_cache.dtype for t in (q, k, v, v_cache, q_out, kt)):
+        raise TypeError("%s: tensors and cache must be of one type" % name)
+    B, N, Hkv, d = k.shape
+    if q is not None and cos_sin is None:
+        raise ValueError("%s: q without cos_sin: nothing would be done to it" % name)
+    qs = qos = kos = (0, 0, 0)
+    Hq = Hkv
+    if q is not None:
+        Hq = q.shape[2]
+        qs = _rows("q", q, B, N, Hq, d)
+        if q_out is None:
+            q_out = _empty_like(q, stream)
+        qos = _rows("q_out", q_out, B, N, Hq, d)
+    elif q_out is not None:
+        raise ValueError("%s: q_out without q" % name)
+    if k_out is True:
+        kt = _empty_like(k, stream)
+    if kt is not None:
+        kos = _rows("k_out", kt, B, N, Hkv, d)
+    table = _ints("block_table", block_table, B, None)
+    p = bsfa_append(B, Hq, N, *qs, *_rows("k", k, B, N, Hkv, d), *_rows("v", v, B, N, Hkv, d), *qos, *kos,
+                    None if seqlens is None else _ints("seqlens", seqlens, B), _ints("start", start, B), table,
+                    block_table.stride(0), block_table.shape[1], None, 0, 0, int(bool(interleaved)))
+    if cos_sin is not None:
+        if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
+            raise TypeError("%s: cos_sin must be contiguous float32 [positions, rot_dim]" % name)
+        p.cos_sin, p.n_positions, p.rot_dim = cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1]
+    _on_device(k.device, lib().bsfa_cache_append, ctypes.byref(c), ctypes.byref(p), None if q is None else q.data_ptr(),
+               k.data_ptr(), v.data_ptr(), None if q is None else q_out.data_ptr(), None if kt is None else kt.data_ptr(),
+               _raw_stream(stream, k.device))
+    return q_out, kt
+
+
+def _empty_like(t, stream):
+    if stream is None:
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _paged_problem(name, q, k_cache, v_cache, prefix_table, prefix_len, block_table, cache_lens, q_lens, out, lse, max_cache_len, stream):
+    _same_device(name, q, k_cache, v_cache, prefix_table, block_table, cache_lens, q_lens, out, lse)
+    c = _cache(name, k_cache, v_cache)
+    if q.dim() != 4 or q.shape[3] != k_cache.shape[3]:
+        raise ValueError("%s: q must be [B, N, Hq, d] with the cache's d" % name)
+    if out is None:
+        out = _empty_like(q, stream)
+    if q.dtype != k_cache.dtype or v_cache.dtype != q.dtype or out.dtype != q.dtype:
+        raise TypeError("%s: tensors and cache must be of one type" % name)
+    B, N, Hq, d = q.shape
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, N, Hq) or not lse.is_contiguous()):
+        raise TypeError("%s: lse must be contiguous float32 [B, N, Hq]" % name)
+    p = bsfa_paged(B, Hq, N, *_rows("q", q, B, N, Hq, d), *_rows("out", out, B, N, Hq, d),
+                   None if q_lens is None else _ints("q_lens", q_lens, B), _ints("cache_lens", cache_lens, B),
+                   _ints("block_table", block_table, B, None), block_table.stride(0), block_table.shape[1], int(max_cache_len))
+    if prefix_table is not None:
+        p.prefix_table, p.prefix_len, p.prefix_pages = _ints("prefix_table", prefix_table, None), int(prefix_len), prefix_table.shape[0]
+    return c, p, out
+
+
+def _attend(call, c, p, q, causal, out, lse, workspace, stream):
+    cref, pref = ctypes.byref(c), ctypes.byref(p)
+    if workspace is True:
+        need = lib().bsfa_paged_workspace_bytes(cref, pref)
+        workspace = _scratch(need, q.device, stream) if need else None
+    if workspace is not None and workspace is not False:
+        _same_device("bsfa", q, workspace)
+        p.workspace = workspace.data_ptr()
+        p.workspace_bytes = workspace.numel() * workspace.element_size()
+    _on_device(q.device, call, cref, pref, q.data_ptr(), 1 if causal else 0, out.data_ptr(),
+               None if lse is None else lse.data_ptr(), _raw_stream(stream, q.device))
+    return out
+
+
+def bsfa_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+                         cache_lens: torch.Tensor, q_lens: Optional[torch.Tensor] = None, causal: bool = True,
+                         out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, max_cache_len: int = 0,
+                         workspace=True, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """out = attention of the new tokens q [B,N,Hq,d] over a paged cache [n_pages, page_size, Hkv, d]: element b's
+    cache_lens[b] tokens (int32 GPU tensor [B]) lie in the pages of block_table[b] (int32), its new tokens are the last
+    q_lens[b] of them (default N; rows behind that are left alone) and see, if ``causal``, the places up to their own, else
+    all.  ``lse``: fp32 [B,N,Hq], written if given.  ``max_cache_len``: a bound of the lengths that the host may know.
+    ``workspace``: a uint8 GPU tensor of paged_workspace_bytes(...) bytes (calls that overlap need one each), or True
+    (scratch memory of the call's own).  Enqueues on ``stream`` (default: torch's current stream)."""
+    c, p, out = _paged_problem("bsfa_paged_attention", q, k_cache, v_cache, None, 0, block_table, cache_lens, q_lens, out, lse, max_cache_len, stream)
+    return _attend(lib().bsfa_paged_attention, c, p, q, causal, out, lse, workspace, stream)
+
+
+def bsfa_prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, prefix_table: torch.Tensor,
+                          prefix_len: int, block_table: torch.Tensor, cache_lens: torch.Tensor,
+                          q_lens: Optional[torch.Tensor] = None, causal: bool = True, out: Optional[torch.Tensor] = None,
+                          lse: Optional[torch.Tensor] = None, max_cache_len: int = 0, workspace=True,
+                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """bsfa_paged_attention for a batch whose elements share the ``prefix_len`` tokens in the pages of ``prefix_table``
+    (int32 GPU tensor): every new token sees them, before its element's own, which alone block_table and cache_lens
+    count.  The prefix is read once for the batch."""
+    c, p, out = _paged_problem("bsfa_prefix_attention", q, k_cache, v_cache, prefix_table, prefix_len, block_table, cache_lens, q_lens, out, lse, max_cache_len, stream)
+    return _attend(lib().bsfa_prefix_attention, c, p, q, causal, out, lse, workspace, stream)
+
+
+def paged_workspace_bytes(q: torch.Tensor, k_cache: torch.Tensor, block_table: torch.Tensor, prefix_table: Optional[torch.Tensor] = None,
+                          prefix_len: int = 0, max_cache_len: int = 0) -> int:
+    """Bytes of workspace bsfa_paged_attention (with prefix_table: bsfa_prefix_attention) needs for these shapes."""
+    lens = torch.empty(q.shape[0], dtype=torch.int32, device=q.device)
+    c, p, _ = _paged_problem("paged_workspace_bytes", q, k_cache, k_cache, prefix_table, prefix_len, block_table, lens, None, q, None, max_cache_len, None)
+    return int(lib().bsfa_paged_workspace_bytes(ctypes.byref(c), ctypes.byref(p)))
 
 
 def bsfa_query_build():

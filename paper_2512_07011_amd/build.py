@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libbsfa.so")
 # translation units: (source, extra flags).  bsfa_fwd.hip is compiled once per group of kernel instantiations.
 FWD_PARTS = 11
 UNITS = [("bsfa_fwd.hip", ["-DBSFA_PART=%d" % i]) for i in range(FWD_PARTS)] + \
-        [(s, []) for s in ("bsfa_select.hip", "bsfa_probe.hip", "bsfa_api.hip")]
+        [(s, []) for s in ("bsfa_select.hip", "bsfa_probe.hip", "bsfa_cache.hip", "bsfa_paged.hip", "bsfa_cache_api.hip", "bsfa_api.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # accumulators in plain VGPRs: kernels whose LDS leaves room for one wave per SIMD would otherwise be given

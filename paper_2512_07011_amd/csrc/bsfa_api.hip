@@ -15,6 +15,19 @@ namespace {
 
 thread_local char g_err[512] = "";
 
+}  // namespace
+
+int bsfa::fail_with(int status, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof(g_err), fmt, ap);
+    va_end(ap);
+    return status;
+}
+
+namespace {
+
 bsfa_status fail(bsfa_status s, const char *fmt, ...)
 {
     va_list ap;

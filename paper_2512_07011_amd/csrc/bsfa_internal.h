@@ -29,6 +29,9 @@ inline FastDiv fast_div(uint32_t d)               // 1 <= d < 2^31
 // million items on (15 to a row), which no sequence that fits the card's memory has, but nothing else keeps out.
 __host__ __device__ inline int counted_row(int sum, int x, int k) { return (int)((uint32_t)(sum - x - 1) / (uint32_t)k); }
 
+// Notes the message that bsfa_last_error returns, and passes `status` on (a bsfa_status).
+int fail_with(int status, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+
 struct FwdParams {
     const uint16_t *q, *k, *v;       // bf16 or fp16 bit patterns (f16 says which)
     uint16_t *out;
@@ -97,6 +100,48 @@ struct TopkLevels {
 // for k = 0.  Enqueues on stream.
 hipError_t launch_topk(const float *dump, int mkv, long row0, long n_rows, const TopkLevels &lv, int n_lv, float *out_dev,
                        hipStream_t stream);
+
+// ---- paged K/V cache (bsfa_cache.hip, bsfa_paged.hip) ------------------------------------------------
+// Element strides in and between the pages of a cache; token t of a sequence lies in page table[t >> page_log2], at place
+// t & (page - 1).  Page ids outside [0, n_pages) hold nothing.
+struct PageLayout {
+    int64_t ksp, ksn, ksh, vsp, vsn, vsh;
+    int page_log2, n_pages;
+};
+
+struct AppendParams {
+    const uint16_t *q, *k, *v;       // q null: keys and values only
+    uint16_t *q_out, *k_out;         // k_out null: keys go to the cache only
+    uint16_t *k_cache, *v_cache;
+    PageLayout pages;
+    const int32_t *seqlens, *start;  // [batch]; seqlens null: all have seqlen
+    const int32_t *table;            // [batch] rows of table_pages page ids, tsb apart
+    const float *cos_sin;            // [positions][rot], or null: nothing is rotated
+    int64_t qsb, qsn, qsh, ksb, ksn, ksh, vsb, vsn, vsh, qosb, qosn, qosh, kosb, kosn, kosh, tsb;
+    int batch, seqlen, hq, hkv, table_pages, rot, interleaved;
+    FastDiv div_seqlen;              // set by the launch
+};
+hipError_t launch_append(const AppendParams &p, int head_dim, bool f16, hipStream_t stream);
+
+struct PagedParams {
+    const uint16_t *q, *k_cache, *v_cache;
+    uint16_t *out;
+    float *lse;                      // [batch][seqlen][hq] or null
+    PageLayout pages;
+    const int32_t *cache_lens;       // [batch]
+    const int32_t *q_lens;           // [batch] or null (all have seqlen)
+    const int32_t *table;            // [batch] rows of page ids, tsb apart
+    const int32_t *prefix_table;     // page ids of the tokens that all elements share, or null
+    int64_t qsb, qsn, qsh, osb, osn, osh, tsb;
+    int batch, seqlen, hq, hkv, group;
+    int max_len;                     // lengths are clamped to it
+    int prefix;                      // tokens of the shared prefix, 0: none
+    int causal;
+    float scale_log2;                // log2(e)/sqrt(d)
+    unsigned char *workspace;        // paged_workspace_bytes, 256-byte aligned; null where that is 0
+};
+size_t paged_workspace_bytes(const PagedParams &p, int head_dim);
+hipError_t launch_paged(const PagedParams &p, int head_dim, bool f16, hipStream_t stream);
 
 // ---- matrix-instruction rate probe (bsfa_probe.hip) --------------------------------------------
 constexpr int kProbeThreads = 512;        // 8 waves per workgroup: two per SIMD, as the forward kernel runs
