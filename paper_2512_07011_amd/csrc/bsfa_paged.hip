@@ -107,17 +107,25 @@ template <int D> struct SubBlock {
             off[u] = (uint32_t)(row * (int)stride + ((lane % (D / 8)) ^ swizzle<D>(row)) * 8) * 2u;
         }
     }
-    // requests the sub-block whose first row is at `src`; of its rows only `n` exist, the others become 0
-    __device__ __forceinline__ static void copy(const uint16_t *src, int n, int64_t stride, const uint32_t (&off)[UNITS], uint32_t lds)
+    // of the sub-block whose first row is at `src`; of its rows only `n` exist, the others become 0
+    __device__ __forceinline__ static i32x4 descriptor(const uint16_t *src, int n, int64_t stride)
     {
         const uint64_t at = reinterpret_cast<uint64_t>(src);
         const i32x4 rsrc = {(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffffu), n > 0 ? ((n - 1) * (int)stride + D) * 2 : 0, 0x00020000};
-        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds);
         asm volatile("s_nop 3" : : "s"(rsrc));           // (a descriptor from a vector instruction is read 5 states later at the earliest)
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u)
-            asm volatile("s_add_u32 m0, %1, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %3, 0 offen lds"
-                         : : "v"(off[u]), "s"(dst), "n"(u * kUnit), "s"(rsrc) : "memory", "m0", "scc");
+        return rsrc;
+    }
+    // requests unit U into the sub-block's place `dst`, which is uniform
+    template <int U> __device__ __forceinline__ static void unit(i32x4 rsrc, uint32_t off, uint32_t dst)
+    {
+        asm volatile("s_add_u32 m0, %1, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %3, 0 offen lds"
+                     : : "v"(off), "s"(dst), "n"(U * kUnit), "s"(rsrc) : "memory", "m0", "scc");
+    }
+    __device__ __forceinline__ static void copy(const uint16_t *src, int n, int64_t stride, const uint32_t (&off)[UNITS], uint32_t lds)
+    {
+        const i32x4 rsrc = descriptor(src, n, stride);
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds);
+        static_for<UNITS>([&](auto u) { unit<decltype(u)::value>(rsrc, off[decltype(u)::value], dst); });
     }
 };
 
@@ -237,7 +245,7 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
         return y;
     };
     // keys of a sub-block that exist: none where it lies behind the range or its page is none of the cache's
-    auto exist = [&](int key, int id) { return (unsigned)id < (unsigned)p.pages.n_pages ? min(max(k1 - key, 0), kSub) : 0; };
+    auto exist = [&](int key, int id) { return __builtin_amdgcn_readfirstlane((unsigned)id < (unsigned)p.pages.n_pages ? min(max(k1 - key, 0), kSub) : 0); };
     auto request = [&](int key, const Ids &ids, uint32_t at) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -402,6 +410,319 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
     }
 }
 
+// ---- many rows: keys shared by a workgroup's waves ------------------------------------------------------
+// Four waves of 32 rows on tiles of 64 keys, K and V in two LDS slots each; a wave copies the sub-block of its number.
+//   S^T = K Q^T, O^T += V^T P^T with 32x32x16 MFMA, P in registers as above.
+// One barrier a tile, between the halves of a stage:
+//   stage j:  P_j = 2^(S_j - m) (VALU) between the MFMAs of S_{j+1}; the copies of K_{j+2} and V_j have landed; barrier;
+//             the MFMAs of O with, between them, the requests for K_{j+3} and V_{j+1} and the row maxima of S_{j+1}
+// Two workgroups on a CU hide each other's barriers.
+constexpr int kTileRows = 128, kTileKeys = 64;
+
+template <int D, bool F16, bool PREFIX>
+__global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
+{
+    typedef typename Elem<F16>::T el;
+    typedef typename Elem<F16>::x8 el8;
+    typedef SubBlock<D> SB;
+    constexpr int KS = D / 16, DB = D / 32;              // MFMAs of a score half; 32-row blocks of O^T
+    constexpr int NQK = 2 * KS, NPV = 4 * DB, EPM = 32 / NQK;
+    constexpr int PD = 4;                                // operand reads run that many MFMAs ahead
+    constexpr int SLOT = 4 * SB::BYTES;
+    constexpr uint32_t K0 = 0, V0 = 2 * SLOT;
+    __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * SLOT];
+
+    const PagedParams &p = a.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hk = blockIdx.x % p.hkv, w = blockIdx.x / p.hkv;
+    const int rg = a.groups - 1 - w % a.groups, x = w / a.groups;      // later rows see more keys: first
+    Range r;
+    int qn = p.seqlen, k0, k1;
+    if constexpr (PREFIX) {
+        r.b = 0, r.part = x, r.parts = a.parts, r.first = 0, r.len = p.prefix;
+        k0 = x * a.chunk;
+        k1 = min(p.prefix, k0 + a.chunk);
+    } else {
+        if (!find_range<true>(a, x, r)) return;
+        qn = __builtin_amdgcn_readfirstlane(queries_of(p, r.b));
+        k0 = r.part * r.chunk;
+        k1 = (int)min((int64_t)r.len, (int64_t)k0 + r.chunk);
+    }
+    const int row0 = rg * kTileRows;
+    if (!PREFIX && row0 >= qn * p.group && a.direct && r.parts == 1) return;         // (no row to store)
+    const int l32 = lane & 31, hh = lane >> 5;
+    const Row mine = row_of<PREFIX>(a, row0 + wave * 32 + l32, r.b, hk);
+    int sees = k1, all_see = k1;
+    if (!PREFIX && p.causal) {
+        sees = min(k1, r.len - qn + mine.i + 1);
+        all_see = min(k1, r.len - qn + (row0 + wave * 32) / p.group + 1);             // (of this wave's rows)
+        k1 = min(k1, r.len - qn + min(row0 + kTileRows - 1, a.rows - 1) / p.group + 1);
+    }
+    const int n_tiles = max(0, (k1 - k0 + kTileKeys - 1) / kTileKeys);
+
+    const int32_t *table = PREFIX ? p.prefix_table : p.table + r.b * p.tsb;
+    const int last_page = max(k1 - 1, 0) >> p.pages.page_log2, in_page = (1 << p.pages.page_log2) - 1;
+    el8 q[KS];
+    {
+        const uint16_t *src = p.q + mine.b * p.qsb + mine.i * p.qsn + mine.h * p.qsh + hh * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const el8 *>(src + 16 * s);
+    }
+    uint32_t koff[SB::UNITS], voff[SB::UNITS];
+    SB::offsets(koff, lane, p.pages.ksn);
+    SB::offsets(voff, lane, p.pages.vsn);
+    const uint32_t lds = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)ring);
+    const uint16_t *const kh = p.k_cache + hk * p.pages.ksh, *const vh = p.v_cache + hk * p.pages.vsh;
+
+    // the pages of a tile's sub-blocks, and of this wave's
+    struct Tile { int id[4], mine; };
+    auto tile_of = [&](int t) {
+        Tile y;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) y.id[s] = page_id(table, k0 + t * kTileKeys + s * kSub, p.pages.page_log2, last_page);
+        y.mine = page_id(table, k0 + t * kTileKeys + wave * kSub, p.pages.page_log2, last_page);
+        return y;
+    };
+    auto in_cache = [&](int id) { return (unsigned)id < (unsigned)p.pages.n_pages; };
+    struct Source { i32x4 rsrc; uint32_t dst; };
+    auto source = [&](const uint16_t *base, int64_t sp, int64_t sn, int t, const Tile &y, uint32_t slot) {
+        const int key = k0 + t * kTileKeys + wave * kSub;
+        const int n = __builtin_amdgcn_readfirstlane(in_cache(y.mine) ? min(max(k1 - key, 0), kSub) : 0);
+        const int64_t id = n > 0 ? y.mine : 0;
+        return Source{SB::descriptor(base + id * sp + (key & in_page) * sn, n, sn), (uint32_t)__builtin_amdgcn_readfirstlane(lds + slot + wave * SB::BYTES)};
+    };
+    auto k_source = [&](int t, const Tile &y, uint32_t slot) { return source(kh, p.pages.ksp, p.pages.ksn, t, y, K0 + slot); };
+    auto v_source = [&](int t, const Tile &y, uint32_t slot) { return source(vh, p.pages.vsp, p.pages.vsn, t, y, V0 + slot); };
+
+    // operand addresses.  K: row 32 kb + l32, elements 16 s + 8 hh .. + 7.  V: keys 16 u + 4 hh + 8 half + (L >> 2), 4 elements
+    // from G16 * g16 + X * x + 4 (L & 3) on, transposed within 16 lanes: operand row 16 g16 + L of block x is that element of O
+    constexpr int G16 = D == 128 ? 64 : 16, X = D == 128 ? 16 : 32;
+    const int L = lane & 15, g16 = (lane >> 4) & 1;
+    uint32_t ka[KS], va[DB][2];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) ka[s] = lds + (l32 >> 4) * SB::BYTES + (l32 & 15) * (D * 2) + (((2 * s + hh) ^ swizzle<D>(l32 & 15)) * 16);
+#pragma unroll
+    for (int y = 0; y < DB; ++y)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int row = 4 * hh + 8 * half + (L >> 2), chunk = (G16 * g16 + X * y) / 8 + ((L >> 1) & 1);
+            va[y][half] = lds + row * (D * 2) + ((chunk ^ swizzle<D>(row)) * 16) + (L & 1) * 8;
+        }
+    auto k_operand = [&](int n, uint32_t slot) {         // MFMA n: k-step n / 2, keys 32 (n % 2) ..
+        return *LDS_PTR(const el8, ka[n >> 1] + K0 + slot + (n & 1) * 2 * SB::BYTES);
+    };
+    auto v_operand = [&](int n, uint32_t slot) {         // MFMA n: sub-block n / DB, block n % DB
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, va[n % DB][0] + V0 + slot + n / DB * SB::BYTES));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, va[n % DB][1] + V0 + slot + n / DB * SB::BYTES));
+        return __builtin_bit_cast(el8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+
+    f32x16 o[DB];
+#pragma unroll
+    for (int y = 0; y < DB; ++y)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[y][e] = 0.f;
+    float m = kNone, l = 0.f, alpha = 1.f;
+    uint64_t grown = 0;                                  // lanes whose row's maximum has grown with the next tile
+
+    struct Scores { f32x16 s[2]; };
+    auto masked = [&](Scores &z, int t, const Tile &y) {
+        const int key = k0 + t * kTileKeys;
+        bool there[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) there[s] = in_cache(y.id[s]);
+        if (there[0] & there[1] & there[2] & there[3] & (key + kTileKeys <= all_see)) return;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int y = 32 * kb + 8 * (e >> 2) + 4 * hh + (e & 3);
+                z.s[kb][e] = there[2 * kb + (e >> 3)] & (key + y < sees) ? z.s[kb][e] : -INFINITY;
+            }
+    };
+    auto new_max = [&](float mx) {                       // of the raw scores, in both lanes of the row
+        const float y = fmaxf(m, mx * p.scale_log2);
+        grown = __builtin_amdgcn_ballot_w64(y > m);
+        alpha = __builtin_amdgcn_exp2f(m - y);
+        l *= alpha;
+        m = y;
+    };
+    auto prob = [&](const Scores &z, int n) { return __builtin_amdgcn_exp2f(fmaf(z.s[n >> 4][n & 15], p.scale_log2, -m)); };
+
+    el8 kpre[PD];
+    Tile t1, t2, t3;                                     // pages of tiles j + 1, j + 2, j + 3
+    // Stage j on the slots of its parity: cur -> P, next <- scores of tile j + 1, if there is one.
+    auto stage = [&](auto parity, auto last, Scores &cur, Scores &next, int j) {
+        constexpr uint32_t S0 = decltype(parity)::value * SLOT, S1 = SLOT - S0;      // slots of tile j and j + 1
+        constexpr bool LAST = decltype(last)::value;
+        el8 pr[4];
+        float ex[EPM], sum[2] = {0.f, 0.f};
+        auto pack = [&](int n) {
+#pragma unroll
+            for (int t = 0; t < EPM; ++t) pr[(n * EPM + t) >> 3][(n * EPM + t) & 7] = (el)ex[t];
+        };
+        if constexpr (!LAST) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) next.s[kb][e] = 0.f;
+        }
+        el8 ops[NQK + PD];
+#pragma unroll
+        for (int n = 0; n < PD; ++n) ops[n] = kpre[n];
+#pragma unroll
+        for (int n = 0; n < NQK; ++n) {
+            if constexpr (!LAST) {
+                if (n + PD < NQK) ops[n + PD] = k_operand(n + PD, S1);
+                next.s[n & 1] = mfma16(ops[n], q[n >> 1], next.s[n & 1]);
+            }
+            float nx[EPM];
+#pragma unroll
+            for (int t = 0; t < EPM; ++t) nx[t] = prob(cur, n * EPM + t);
+            if (n > 0) pack(n - 1);
+#pragma unroll
+            for (int t = 0; t < EPM; ++t) {
+                ex[t] = nx[t];
+                sum[t & 1] += nx[t];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        pack(NQK - 1);
+        l += sum[0] + sum[1];
+        Tile t4;
+        if constexpr (!LAST) {
+            masked(next, j + 1, t1);
+            t4 = tile_of(j + 4);
+        }
+        wait_vmcnt<0>();
+        wg_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        el8 vo[NPV + PD];
+#pragma unroll
+        for (int n = 0; n < PD; ++n) vo[n] = v_operand(n, S0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (grown) {
+#pragma unroll
+            for (int y = 0; y < DB; ++y)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[y][e] *= alpha;
+        }
+        Source ks, vs;
+        if constexpr (!LAST) {
+            ks = k_source(j + 3, t3, S1);
+            vs = v_source(j + 1, t1, S1);
+            t1 = t2;
+            t2 = t3;
+            t3 = t4;
+        }
+        float mx = -INFINITY;
+        static_for<NPV>([&](auto nc) {
+            constexpr int n = decltype(nc)::value;
+            if constexpr (n + PD < NPV) vo[n + PD] = v_operand(n + PD, S0);
+            o[n % DB] = mfma16(vo[n], pr[n / DB], o[n % DB]);
+            if constexpr (!LAST) {
+                constexpr int PER = 2 * SB::UNITS / (NPV / 2);         // requests behind the first half of the MFMAs
+                if constexpr (n < NPV / 2)
+                    static_range<n * PER, (n + 1) * PER>([&](auto cc) {
+                        constexpr int c = decltype(cc)::value, u = c % SB::UNITS;
+                        if constexpr (c < SB::UNITS) SB::template unit<u>(vs.rsrc, voff[u], vs.dst);
+                        else SB::template unit<u>(ks.rsrc, koff[u], ks.dst);
+                    });
+                constexpr int QUARTER = 32 / (NPV / 4);                // scores of a slot of the second quarter on
+                if constexpr (n >= NPV / 4 && n < NPV / 2)
+#pragma unroll
+                    for (int e = (n - NPV / 4) * QUARTER; e < (n - NPV / 4 + 1) * QUARTER; ++e) mx = fmaxf(mx, next.s[e >> 4][e & 15]);
+                if constexpr (n == NPV / 2) mx = pair_max(mx);
+                if constexpr (n == NPV / 2 + 1) new_max(mx);
+                if constexpr (n == NPV - 2)
+#pragma unroll
+                    for (int y = 0; y < PD; ++y) kpre[y] = k_operand(y, S0);          // of tile j + 2
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+
+    if (n_tiles > 0) {
+        const Tile t0 = tile_of(0);
+        t1 = tile_of(1);
+        t2 = tile_of(2);
+        t3 = tile_of(3);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));      // (the queries before the copies: their wait would wait for both)
+        auto whole = [&](const Source &s, const uint32_t (&off)[SB::UNITS]) {
+            static_for<SB::UNITS>([&](auto u) { SB::template unit<decltype(u)::value>(s.rsrc, off[decltype(u)::value], s.dst); });
+        };
+        whole(k_source(0, t0, 0), koff);
+        whole(k_source(1, t1, SLOT), koff);
+        whole(v_source(0, t0, 0), voff);
+        wait_vmcnt<2 * SB::UNITS>();
+        wg_barrier();
+        Scores even, odd;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) even.s[kb][e] = 0.f;
+#pragma unroll
+        for (int n = 0; n < NQK; ++n) even.s[n & 1] = mfma16(k_operand(n, 0), q[n >> 1], even.s[n & 1]);
+        masked(even, 0, t0);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) mx = fmaxf(mx, even.s[e >> 4][e & 15]);
+        new_max(pair_max(mx));
+        grown = 0;                                       // (the accumulators are zero)
+        wait_vmcnt<0>();
+        wg_barrier();
+        whole(k_source(2, t2, 0), koff);
+#pragma unroll
+        for (int y = 0; y < PD; ++y) kpre[y] = k_operand(y, SLOT);
+        // (two stages to a turn, so that the slots are constants; the last of an even number looks ahead to a tile of nothing)
+        for (int j = 0; j + 1 < n_tiles; j += 2) {
+            stage(std::integral_constant<int, 0>{}, std::false_type{}, even, odd, j);
+            stage(std::integral_constant<int, 1>{}, std::false_type{}, odd, even, j + 1);
+        }
+        if (n_tiles & 1) stage(std::integral_constant<int, 0>{}, std::true_type{}, even, odd, n_tiles - 1);
+    }
+
+    // ---- results, through the LDS so that rows are written in whole lines ---------------------------------------
+    wg_barrier();
+    l += __shfl_xor(l, 32);
+    const bool direct = !PREFIX && a.direct && r.parts == 1;
+    const float f = !direct ? 1.f : l > 0.f ? 1.f / l : 0.f;
+    constexpr int CH = D / 4;                            // 16-byte chunks of a row of 32-bit results
+    float *const ro = reinterpret_cast<float *>(ring) + wave * 32 * D;
+#pragma unroll
+    for (int y = 0; y < DB; ++y)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int d = D == 128 ? 16 * y + 64 * (c >> 1) + 8 * (c & 1) + 4 * hh : 32 * y + 8 * c + 4 * hh;
+            *reinterpret_cast<f32x4 *>(ro + l32 * D + (((d >> 2) ^ (l32 % CH)) << 2)) =
+                f32x4{o[y][4 * c] * f, o[y][4 * c + 1] * f, o[y][4 * c + 2] * f, o[y][4 * c + 3] * f};
+        }
+    if (hh == 0) {
+        const int row = row0 + wave * 32 + l32;
+        if (direct) {
+            if (p.lse && mine.stored && mine.i < qn)
+                p.lse[((int64_t)mine.b * p.seqlen + mine.i) * p.hq + mine.h] = l > 0.f ? 0.6931471805599453f * (m + __builtin_amdgcn_logf(l)) : -INFINITY;
+        } else if (mine.stored)
+            (PREFIX ? a.prefix_ml : a.own_ml)[((int64_t)(PREFIX ? x : r.first + r.part) * p.hkv + hk) * a.rows + row] = make_float2(m, l);
+    }
+    constexpr int AT_ONCE = 64 / CH;                     // rows
+    for (int y = lane / CH; y < 32; y += AT_ONCE) {
+        const int row = row0 + wave * 32 + y, c = lane % CH;
+        const Row z = row_of<PREFIX>(a, row, r.b, hk);
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(ro + y * D + ((c ^ (y % CH)) << 2));
+        if (!z.stored) continue;
+        if (direct) {
+            if (z.i >= qn) continue;
+            typedef el el4 __attribute__((ext_vector_type(4)));
+            *reinterpret_cast<el4 *>(p.out + z.b * p.osb + z.i * p.osn + z.h * p.osh + 4 * c) = el4{(el)v[0], (el)v[1], (el)v[2], (el)v[3]};
+        } else {
+            float *dst = (PREFIX ? a.prefix_o : a.own_o) + (((int64_t)(PREFIX ? x : r.first + r.part) * p.hkv + hk) * a.rows + row) * D;
+            *reinterpret_cast<f32x4 *>(dst + 4 * c) = v;
+        }
+    }
+}
+
 // ---- ranges joined --------------------------------------------------------------------------------------
 // A workgroup is one row of one query head: its waves take the ranges in turn, a lane D / 64 elements.
 template <int D, bool F16>
@@ -460,7 +781,8 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const Launch a, const i
 
 // ---- launch -----------------------------------------------------------------------------------------------
 constexpr int kWaves = 4;
-constexpr int kPlaces = 256;         // workgroups that the chip holds
+constexpr int kPlaces = 256;         // workgroups of the streaming kernel that the chip holds; twice as many of the other
+constexpr int kFewRows = 64;         // up to that many rows of a unit are streamed
 
 static int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
@@ -475,9 +797,10 @@ static Plan plan_of(const PagedParams &p, int head_dim)
     Launch a = {};
     a.p = p;
     a.rows = p.seqlen * p.group;
-    a.groups = (a.rows + 63) / 64;
+    a.groups = a.rows <= kFewRows ? 1 : (a.rows + kTileRows - 1) / kTileRows;
     const int64_t items = (int64_t)p.batch * p.hkv * a.groups;
-    a.extra = p.max_len <= 256 || items >= 4 * kPlaces ? 0 : (int)std::max<int64_t>(1, (4 * kPlaces) / (p.hkv * a.groups));
+    const int places = a.rows <= kFewRows ? 4 * kPlaces : 2 * kPlaces;
+    a.extra = p.max_len <= 256 || items >= places ? 0 : (int)std::max<int64_t>(1, places / (p.hkv * a.groups));
     a.direct = p.prefix == 0;
     y.own = a;
     y.bytes = 0;
@@ -489,8 +812,8 @@ static Plan plan_of(const PagedParams &p, int head_dim)
         Launch &z = y.prefix;
         z = a;
         z.rows = p.batch * a.rows;
-        z.groups = (z.rows + 63) / 64;
-        const int want = (int)std::max<int64_t>(1, 4 * kPlaces / ((int64_t)p.hkv * z.groups));
+        z.groups = z.rows <= kFewRows ? 1 : (z.rows + kTileRows - 1) / kTileRows;
+        const int want = (int)std::max<int64_t>(1, (z.rows <= kFewRows ? 4 : 2) * kPlaces / ((int64_t)p.hkv * z.groups));
         z.chunk = std::max(128, (int)(((int64_t)p.prefix + want - 1) / want + 127) / 128 * 128);
         z.parts = (p.prefix + z.chunk - 1) / z.chunk;
         y.own.parts = z.parts;
@@ -514,19 +837,20 @@ static Plan plan_of(const PagedParams &p, int head_dim)
 
 size_t paged_workspace_bytes(const PagedParams &p, int head_dim) { return (size_t)plan_of(p, head_dim).bytes; }
 
-template <int D, bool F16, bool PREFIX> static void stream_keys(const Launch &a, int64_t ranges, hipStream_t stream)
+template <int D, bool F16, bool PREFIX> static void attend(const Launch &a, int64_t ranges, hipStream_t stream)
 {
     const unsigned grid = (unsigned)(ranges * a.p.hkv * a.groups);
     if (a.rows <= 16) paged_stream_kernel<D, kWaves, 1, F16, PREFIX><<<grid, kWaves * 64, 0, stream>>>(a);
     else if (a.rows <= 32) paged_stream_kernel<D, kWaves, 2, F16, PREFIX><<<grid, kWaves * 64, 0, stream>>>(a);
-    else paged_stream_kernel<D, kWaves, 4, F16, PREFIX><<<grid, kWaves * 64, 0, stream>>>(a);
+    else if (a.rows <= kFewRows) paged_stream_kernel<D, kWaves, 4, F16, PREFIX><<<grid, kWaves * 64, 0, stream>>>(a);
+    else paged_tile_kernel<D, F16, PREFIX><<<grid, 256, 0, stream>>>(a);
 }
 
 template <int D, bool F16> static hipError_t launch(const PagedParams &p, hipStream_t stream)
 {
     const Plan y = plan_of(p, D);
-    if (p.prefix) stream_keys<D, F16, true>(y.prefix, y.prefix.parts, stream);
-    stream_keys<D, F16, false>(y.own, p.batch + y.own.extra, stream);
+    if (p.prefix) attend<D, F16, true>(y.prefix, y.prefix.parts, stream);
+    attend<D, F16, false>(y.own, p.batch + y.own.extra, stream);
     if (y.own.extra || !y.own.direct)
         paged_join_kernel<D, F16><<<(unsigned)(p.batch * p.seqlen * p.hq), 256, 0, stream>>>(y.own, p.batch * y.own.rows, y.own.rows);
     return hipGetLastError();
