@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -122,12 +123,12 @@ def lib() -> ctypes.CDLL:
         L.bsfa_mfma_rate_probe_flops.restype = ctypes.c_double
         L.bsfa_mfma_rate_probe_flops.argtypes = [ctypes.c_int, ctypes.c_int]
         L.bsfa_cache_append.restype = ctypes.c_int
-        L.bsfa_cache_append.argtypes = [ctypes.POINTER(bsfa_cache), ctypes.POINTER(bsfa_append), vp, vp, vp, vp, vp, vp]
+        L.bsfa_cache_append.argtypes = [vp] * 8
         for f in (L.bsfa_paged_attention, L.bsfa_prefix_attention):
             f.restype = ctypes.c_int
-            f.argtypes = [ctypes.POINTER(bsfa_cache), ctypes.POINTER(bsfa_paged), vp, ctypes.c_int, vp, vp, vp]
+            f.argtypes = [vp, vp, vp, ctypes.c_int, vp, vp, vp]
         L.bsfa_paged_workspace_bytes.restype = ctypes.c_size_t
-        L.bsfa_paged_workspace_bytes.argtypes = [ctypes.POINTER(bsfa_cache), ctypes.POINTER(bsfa_paged)]
+        L.bsfa_paged_workspace_bytes.argtypes = [vp, vp]
         L.bsfa_status_string.restype = ctypes.c_char_p
         L.bsfa_status_string.argtypes = [ctypes.c_int]
         L.bsfa_last_error.restype = ctypes.c_char_p
@@ -376,12 +377,19 @@ def rotary_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="
     return torch.cat([angle.cos(), angle.sin()], dim=1).float()
 
 
+# The descriptors as they lie in memory, filled in one go (a tenth of a ctypes.Structure's time; a small call's is the
+# host's): the members of bsfa_cache, bsfa_append and bsfa_paged in order.
+_PACK_CACHE = struct.Struct("@5i6q2P").pack
+_PACK_APPEND = struct.Struct("@3i15q3PqiP3i").pack
+_PACK_PAGED = struct.Struct("@3i6q3Pq2iP2iPq").pack
+
+
 def _same_device(name, q, *ts):
-    d = q.device
-    if d.type != "cuda":
+    d = q.get_device()
+    if d < 0:
         raise ValueError("bsfa: tensors must live on the GPU")
     for t in ts:
-        if t is not None and t.device != d:
+        if t is not None and t.get_device() != d:
             raise ValueError("%s: tensors must live on one GPU" % name)
 
 
@@ -396,29 +404,38 @@ def _on_device(device, call, *args):
         _check(rc)
 
 
-def _ints(name, t, *shape):
-    """Address of an int32 tensor of the given shape (None: any size), contiguous in its last dimension."""
-    if t.dtype != torch.int32 or t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)) or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise TypeError("%s must be int32 of shape %s, contiguous in its last dimension" % (name, list(shape)))
+def _lens(name, t, n):
+    """Address of a contiguous int32 tensor of n elements."""
+    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous():
+        raise TypeError("%s must be contiguous int32 of shape [%d]" % (name, n))
     return t.data_ptr()
 
 
-def _rows(name, t, *shape):
+def _pages(name, t, n):
+    """Address, row stride and row length of an int32 tensor of n rows, contiguous in its last dimension."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not torch.int32 or len(shape) != 2 or shape[0] != n or (stride[1] != 1 and shape[1] > 1):
+        raise TypeError("%s must be int32 [%d, pages], contiguous in its last dimension" % (name, n))
+    return t.data_ptr(), stride[0], shape[1]
+
+
+def _strides(name, t, shape):
     """Strides of a [B, N, H, d] tensor (batch, token, head)."""
     if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, list(t.shape), list(shape)))
-    st = t.stride()
-    if st[3] != 1:
+    b, n, h, one = t.stride()
+    if one != 1:
         raise ValueError("%s: head dimension must be contiguous" % name)
-    return st[:3]
+    return b, n, h
 
 
 def _cache(name, k_cache, v_cache):
-    if k_cache.dim() != 4 or k_cache.dtype not in DTYPES:
-        raise TypeError("%s: k_cache must be [n_pages, page_size, n_kv_heads, head_dim], bfloat16 or float16" % name)
-    shape = k_cache.shape
-    return bsfa_cache(*shape, DTYPES[k_cache.dtype], *_rows("k_cache", k_cache, *shape), *_rows("v_cache", v_cache, *shape),
-                      k_cache.data_ptr(), v_cache.data_ptr())
+    """Descriptor of the cache, its shape and its type."""
+    shape, dtype = k_cache.shape, k_cache.dtype
+    if len(shape) != 4 or dtype not in DTYPES or v_cache.dtype is not dtype:
+        raise TypeError("%s: k_cache and v_cache must be [n_pages, page_size, n_kv_heads, head_dim], both bfloat16 or both float16" % name)
+    return _PACK_CACHE(*shape, DTYPES[dtype], *_strides("k_cache", k_cache, shape), *_strides("v_cache", v_cache, shape),
+                       k_cache.data_ptr(), v_cache.data_ptr()), shape, dtype
 
 
 def bsfa_cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -434,44 +451,46 @@ def bsfa_cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
     rotated keys: what bsfa_forward takes for a prompt; else None.  Enqueues on ``stream`` (default: torch's current
     stream)."""
     name = "bsfa_cache_append"
-    kt = k_out if isinstance(k_out, torch.Tensor) else None
-    _same_device(name, k, q, v, k_cache, v_cache, block_table, start, cos_sin, seqlens, q_out, kt)
-    c = _cache(name, k_cache, v_cache)
-    if k.dim() != 4 or (q is not None and q.dim() != 4):
-        raise ValueError("%s: q, k and v must be [B, N, H, d]" % name)
-    if k.shape[2:] != k_cache.shape[2:]:
-        raise ValueError("%s: k has heads %s, the cache %s" % (name, list(k.shape[2:]), list(k_cache.shape[2:])))
-    if any(t is not None and t.dtype != k_cache.dtype for t in (q, k, v, v_cache, q_out, kt)):
+    if k_out is True:
+        k_out = _empty_like(k, stream)
+    _same_device(name, k, q, v, k_cache, v_cache, block_table, start, cos_sin, seqlens, q_out, k_out)
+    c, (_, _, Hkv, d), dtype = _cache(name, k_cache, v_cache)
+    shape = k.shape
+    if len(shape) != 4 or shape[2] != Hkv or shape[3] != d:
+        raise ValueError("%s: k has shape %s, expected [B, N, %d, %d]" % (name, list(shape), Hkv, d))
+    if k.dtype is not dtype or v.dtype is not dtype or (k_out is not None and k_out.dtype is not dtype):
         raise TypeError("%s: tensors and cache must be of one type" % name)
-    B, N, Hkv, d = k.shape
-    if q is not None and cos_sin is None:
-        raise ValueError("%s: q without cos_sin: nothing would be done to it" % name)
+    B, N, Hq = shape[0], shape[1], Hkv
     qs = qos = kos = (0, 0, 0)
-    Hq = Hkv
+    q_ptr = qo_ptr = ko_ptr = cs_ptr = positions = rot = 0
     if q is not None:
-        Hq = q.shape[2]
-        qs = _rows("q", q, B, N, Hq, d)
+        if cos_sin is None:
+            raise ValueError("%s: q without cos_sin: nothing would be done to it" % name)
+        q_shape = q.shape
+        if len(q_shape) != 4 or q_shape[0] != B or q_shape[1] != N or q_shape[3] != d:
+            raise ValueError("%s: q has shape %s, expected [%d, %d, Hq, %d]" % (name, list(q_shape), B, N, d))
         if q_out is None:
             q_out = _empty_like(q, stream)
-        qos = _rows("q_out", q_out, B, N, Hq, d)
+        if q.dtype is not dtype or q_out.dtype is not dtype:
+            raise TypeError("%s: tensors and cache must be of one type" % name)
+        Hq = q_shape[2]
+        qs, qos = _strides("q", q, q_shape), _strides("q_out", q_out, q_shape)
+        q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("%s: q_out without q" % name)
-    if k_out is True:
-        kt = _empty_like(k, stream)
-    if kt is not None:
-        kos = _rows("k_out", kt, B, N, Hkv, d)
-    table = _ints("block_table", block_table, B, None)
-    p = bsfa_append(B, Hq, N, *qs, *_rows("k", k, B, N, Hkv, d), *_rows("v", v, B, N, Hkv, d), *qos, *kos,
-                    None if seqlens is None else _ints("seqlens", seqlens, B), _ints("start", start, B), table,
-                    block_table.stride(0), block_table.shape[1], None, 0, 0, int(bool(interleaved)))
+    if k_out is not None:
+        kos, ko_ptr = _strides("k_out", k_out, shape), k_out.data_ptr()
     if cos_sin is not None:
-        if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
+        if cos_sin.dtype is not torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
             raise TypeError("%s: cos_sin must be contiguous float32 [positions, rot_dim]" % name)
-        p.cos_sin, p.n_positions, p.rot_dim = cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1]
-    _on_device(k.device, lib().bsfa_cache_append, ctypes.byref(c), ctypes.byref(p), None if q is None else q.data_ptr(),
-               k.data_ptr(), v.data_ptr(), None if q is None else q_out.data_ptr(), None if kt is None else kt.data_ptr(),
-               _raw_stream(stream, k.device))
-    return q_out, kt
+        (positions, rot), cs_ptr = cos_sin.shape, cos_sin.data_ptr()
+    table, table_stride, pages = _pages("block_table", block_table, B)
+    p = _PACK_APPEND(B, Hq, N, *qs, *_strides("k", k, shape), *_strides("v", v, shape), *qos, *kos,
+                     0 if seqlens is None else _lens("seqlens", seqlens, B), _lens("start", start, B), table, table_stride, pages,
+                     cs_ptr, positions, rot, 1 if interleaved else 0)
+    device = k.device
+    _on_device(device, lib().bsfa_cache_append, c, p, q_ptr, k.data_ptr(), v.data_ptr(), qo_ptr, ko_ptr, _raw_stream(stream, device))
+    return q_out, k_out
 
 
 def _empty_like(t, stream):
@@ -481,37 +500,44 @@ def _empty_like(t, stream):
         return torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
-def _paged_problem(name, q, k_cache, v_cache, prefix_table, prefix_len, block_table, cache_lens, q_lens, out, lse, max_cache_len, stream):
+def _attend(call, name, q, k_cache, v_cache, prefix_table, prefix_len, block_table, cache_lens, q_lens, causal, out, lse, max_cache_len, workspace,
+            stream):
+    """The two entry points' common part; call None: the bytes of workspace they need."""
     _same_device(name, q, k_cache, v_cache, prefix_table, block_table, cache_lens, q_lens, out, lse)
-    c = _cache(name, k_cache, v_cache)
-    if q.dim() != 4 or q.shape[3] != k_cache.shape[3]:
-        raise ValueError("%s: q must be [B, N, Hq, d] with the cache's d" % name)
+    c, (_, _, _, d), dtype = _cache(name, k_cache, v_cache)
+    shape = q.shape
+    if len(shape) != 4 or shape[3] != d:
+        raise ValueError("%s: q has shape %s, expected [B, N, Hq, %d]" % (name, list(shape), d))
     if out is None:
         out = _empty_like(q, stream)
-    if q.dtype != k_cache.dtype or v_cache.dtype != q.dtype or out.dtype != q.dtype:
+    if q.dtype is not dtype or out.dtype is not dtype:
         raise TypeError("%s: tensors and cache must be of one type" % name)
-    B, N, Hq, d = q.shape
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, N, Hq) or not lse.is_contiguous()):
-        raise TypeError("%s: lse must be contiguous float32 [B, N, Hq]" % name)
-    p = bsfa_paged(B, Hq, N, *_rows("q", q, B, N, Hq, d), *_rows("out", out, B, N, Hq, d),
-                   None if q_lens is None else _ints("q_lens", q_lens, B), _ints("cache_lens", cache_lens, B),
-                   _ints("block_table", block_table, B, None), block_table.stride(0), block_table.shape[1], int(max_cache_len))
+    B, N, Hq, _ = shape
+    lse_ptr = prefix = pages_p = 0
+    if lse is not None:
+        if lse.dtype is not torch.float32 or lse.shape != (B, N, Hq) or not lse.is_contiguous():
+            raise TypeError("%s: lse must be contiguous float32 [B, N, Hq]" % name)
+        lse_ptr = lse.data_ptr()
     if prefix_table is not None:
-        p.prefix_table, p.prefix_len, p.prefix_pages = _ints("prefix_table", prefix_table, None), int(prefix_len), prefix_table.shape[0]
-    return c, p, out
-
-
-def _attend(call, c, p, q, causal, out, lse, workspace, stream):
-    cref, pref = ctypes.byref(c), ctypes.byref(p)
-    if workspace is True:
-        need = lib().bsfa_paged_workspace_bytes(cref, pref)
-        workspace = _scratch(need, q.device, stream) if need else None
-    if workspace is not None and workspace is not False:
-        _same_device("bsfa", q, workspace)
-        p.workspace = workspace.data_ptr()
-        p.workspace_bytes = workspace.numel() * workspace.element_size()
-    _on_device(q.device, call, cref, pref, q.data_ptr(), 1 if causal else 0, out.data_ptr(),
-               None if lse is None else lse.data_ptr(), _raw_stream(stream, q.device))
+        pages_p = prefix_table.numel()
+        prefix = _lens("prefix_table", prefix_table, pages_p)
+    table, table_stride, pages = _pages("block_table", block_table, B)
+    members = (B, Hq, N, *_strides("q", q, shape), *_strides("out", out, shape), 0 if q_lens is None else _lens("q_lens", q_lens, B),
+               _lens("cache_lens", cache_lens, B), table, table_stride, pages, max_cache_len, prefix, prefix_len, pages_p)
+    ws_ptr = ws_bytes = 0
+    if workspace is True or call is None:
+        ws_bytes = lib().bsfa_paged_workspace_bytes(c, _PACK_PAGED(*members, 0, 0))
+        if call is None:
+            return ws_bytes
+        if ws_bytes:
+            workspace = _scratch(ws_bytes, q.device, stream)
+            ws_ptr = workspace.data_ptr()
+    elif workspace is not None and workspace is not False:
+        _same_device(name, q, workspace)
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    device = q.device
+    _on_device(device, call, c, _PACK_PAGED(*members, ws_ptr, ws_bytes), q.data_ptr(), 1 if causal else 0, out.data_ptr(), lse_ptr,
+               _raw_stream(stream, device))
     return out
 
 
@@ -525,8 +551,8 @@ def bsfa_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     all.  ``lse``: fp32 [B,N,Hq], written if given.  ``max_cache_len``: a bound of the lengths that the host may know.
     ``workspace``: a uint8 GPU tensor of paged_workspace_bytes(...) bytes (calls that overlap need one each), or True
     (scratch memory of the call's own).  Enqueues on ``stream`` (default: torch's current stream)."""
-    c, p, out = _paged_problem("bsfa_paged_attention", q, k_cache, v_cache, None, 0, block_table, cache_lens, q_lens, out, lse, max_cache_len, stream)
-    return _attend(lib().bsfa_paged_attention, c, p, q, causal, out, lse, workspace, stream)
+    return _attend(lib().bsfa_paged_attention, "bsfa_paged_attention", q, k_cache, v_cache, None, 0, block_table, cache_lens, q_lens, causal,
+                   out, lse, max_cache_len, workspace, stream)
 
 
 def bsfa_prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, prefix_table: torch.Tensor,
@@ -537,16 +563,18 @@ def bsfa_prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch
     """bsfa_paged_attention for a batch whose elements share the ``prefix_len`` tokens in the pages of ``prefix_table``
     (int32 GPU tensor): every new token sees them, before its element's own, which alone block_table and cache_lens
     count.  The prefix is read once for the batch."""
-    c, p, out = _paged_problem("bsfa_prefix_attention", q, k_cache, v_cache, prefix_table, prefix_len, block_table, cache_lens, q_lens, out, lse, max_cache_len, stream)
-    return _attend(lib().bsfa_prefix_attention, c, p, q, causal, out, lse, workspace, stream)
+    if prefix_table is None:
+        raise TypeError("bsfa_prefix_attention: prefix_table is missing")
+    return _attend(lib().bsfa_prefix_attention, "bsfa_prefix_attention", q, k_cache, v_cache, prefix_table, prefix_len, block_table, cache_lens,
+                   q_lens, causal, out, lse, max_cache_len, workspace, stream)
 
 
 def paged_workspace_bytes(q: torch.Tensor, k_cache: torch.Tensor, block_table: torch.Tensor, prefix_table: Optional[torch.Tensor] = None,
                           prefix_len: int = 0, max_cache_len: int = 0) -> int:
     """Bytes of workspace bsfa_paged_attention (with prefix_table: bsfa_prefix_attention) needs for these shapes."""
     lens = torch.empty(q.shape[0], dtype=torch.int32, device=q.device)
-    c, p, _ = _paged_problem("paged_workspace_bytes", q, k_cache, k_cache, prefix_table, prefix_len, block_table, lens, None, q, None, max_cache_len, None)
-    return int(lib().bsfa_paged_workspace_bytes(ctypes.byref(c), ctypes.byref(p)))
+    return int(_attend(None, "paged_workspace_bytes", q, k_cache, k_cache, prefix_table, prefix_len, block_table, lens, None, True, q, None, max_cache_len,
+                       True, None))
 
 
 def bsfa_query_build():

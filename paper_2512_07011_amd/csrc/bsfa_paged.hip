@@ -16,83 +16,147 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ f32x4 mfma32(bf16x8_t a, bf16x8_t b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mfma32(f16x8_t a, f16x8_t b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
+__device__ __forceinline__ f32x4 mfma16x16(s16x4 a, Elem<false>::x4 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, __builtin_bit_cast(s16x4, b), c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma16x16(s16x4 a, Elem<true>::x4 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(Elem<true>::x4, a), b, c, 0, 0, 0); }
+
 constexpr float kNone = -3.0e38f;    // running maximum of a row that has seen no key: finite, below any score
+// A row's running maximum follows its scores only when they have outgrown it by more than this (log2 units): weights stay
+// below 2^8, which costs no precision, and accumulators are hardly ever rescaled (with a growth of nothing allowed, some row of
+// 32 grows in one tile of five over 32K keys).
+constexpr float kSlack = 8.f;
 constexpr int kSub = 16;             // keys that lie in one page whatever its size
+constexpr int kMinShare = 8;         // sub-blocks of a workgroup, at least
 
 struct Launch {
     PagedParams p;
-    int extra;                       // > 0: own tokens are cut into ranges, batch + extra at most; 0: one range a sequence
-    int rows;                        // rows of a unit
-    int groups;                      // row groups of a unit, one to a workgroup
-    int chunk;                       // keys of a range of the prefix
-    int parts;                       // ranges of the prefix
-    float *own_o, *prefix_o;         // unscaled results of ranges: [range][hkv][rows][d] ...
-    float2 *own_ml, *prefix_ml;      // ... and their (m, l)
+    // The sequences' own tokens: a unit of `rows` rows each, `groups` workgroups side by side.  shares > 0: the batch's tokens
+    // are dealt to so many workgroups evenly (even_share); 0: every sequence is cut into `parts` ranges.
+    int rows, groups, shares, parts;
+    // The prefix: one unit of prefix_rows rows, ranges of prefix_chunk keys.
+    int prefix_rows, prefix_groups, prefix_parts, prefix_chunk;
+    // Unscaled results of ranges [slot][hkv][rows][d] and their (m, l); slots: see Range, and the prefix's ranges.
+    float *own_o, *prefix_o;
+    float2 *own_ml, *prefix_ml;
+    int own_slots;
     bool direct;                     // a sequence in one range is written to out at once
 };
 
-// ---- ranges of a batch's own tokens ---------------------------------------------------------------
-// Every range is `chunk` tokens or less; chunk follows from the lengths on the device, so that a captured launch stays
-// even as sequences grow: with chunk >= total / extra there are at most batch + extra ranges.
+// The kernels' arguments as they lie in constant memory, asked for anew: each part of a kernel reads what it needs when it
+// begins, and what only the end of a range needs takes no scalar registers during its loop.
+typedef const __attribute__((address_space(4))) Launch Args;
+typedef const __attribute__((address_space(4))) PagedParams Params;
+__device__ __forceinline__ Args &arguments()
+{
+    uint64_t at = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(Args *)at;
+}
+// The same number, computed anew by whatever depends on it.
+__device__ __forceinline__ int anew(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// ---- ranges of keys -------------------------------------------------------------------------------------
 struct Range {
-    int b, part, parts, first, len, chunk;               // sequence, which range of how many; number of ranges before the sequence's
+    int b, len;                      // sequence and its tokens
+    int k0, k1;                      // keys
+    int slot;                        // where the result goes ...
+    bool whole;                      // ... unless this is all of the sequence
 };
 
-__device__ __forceinline__ int length_of(const PagedParams &p, int b) { return min(max(p.cache_lens[b], 0), p.max_len); }
-__device__ __forceinline__ int queries_of(const PagedParams &p, int b) { return p.q_lens ? min(max(p.q_lens[b], 0), p.seqlen) : p.seqlen; }
+__device__ __forceinline__ int length_of(Params &p, int b) { return min(max(p.cache_lens[b], 0), p.max_len); }
+__device__ __forceinline__ int queries_of(Params &p, int b) { return p.q_lens ? min(max(p.q_lens[b], 0), p.seqlen) : p.seqlen; }
+// sub-blocks of a sequence; an empty one counts as one, so that somebody writes its result
+__device__ __forceinline__ int units_of(int len) { return max(1, (len + kSub - 1) / kSub); }
 
-// Counts the ranges off, in every wave alike: the sequence that holds range x (by_range) or the sequence x.
-template <bool BY_RANGE> __device__ __forceinline__ bool find_range(const Launch &a, int x, Range &r)
+// The batch's sub-blocks in a row, dealt to `shares` workgroups evenly: workgroup x has those from x * share on, which may
+// begin and end inside sequences.  A workgroup or a sequence begins with every range, so the range of workgroup x in
+// sequence b has slot x + b.  The shares follow from the lengths on the device: a captured launch stays even as sequences
+// grow.
+struct Share {
+    int share;                       // sub-blocks of a workgroup
+    int b, before, len;              // a sequence, the sub-blocks before it, its tokens
+};
+// sum over lanes 0 .. l: inside rows of 16 lanes, then each row's last lane to the rows behind it
+__device__ __forceinline__ int scan_lanes(int x)
 {
-    const PagedParams &p = a.p;
-    r.first = 0;
-    r.part = 0;
-    r.parts = 1;
-    r.b = x;
-    r.chunk = 0x7fffffff;
-    if (a.extra == 0) {
-        r.first = x;
-        r.len = __builtin_amdgcn_readfirstlane(length_of(p, x));
-        return true;
-    }
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);       // row_shr:2
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);       // row_shr:4
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);       // row_shr:8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
+    return x;
+}
+// The sequence that holds sub-block x * share, or (BY_SHARE false) sequence x; every wave for itself.  False: there is none.
+template <bool BY_SHARE> __device__ __forceinline__ bool even_share(Args &a, int x, Share &y)
+{
+    Params &p = a.p;
     const int lane = threadIdx.x & 63;
-    unsigned long long total = 0;
-    for (int b = lane; b < p.batch; b += 64) total += (unsigned)length_of(p, b);
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) total += __shfl_xor(total, s);
-    const unsigned long long even = (total + a.extra - 1) / (unsigned)a.extra;
-    r.chunk = (int)min(max((even + 127) & ~127ull, 128ull), 0x7fffff80ull);
-    r.chunk = __builtin_amdgcn_readfirstlane(r.chunk);
-    int before = 0;
+    auto scan = [&](int b0, int &len, int &upto) {       // sub-blocks of sequences b0 .. b0 + lane
+        len = b0 + lane < p.batch ? length_of(p, b0 + lane) : 0;
+        upto = scan_lanes(b0 + lane < p.batch ? units_of(len) : 0);
+        return __builtin_amdgcn_readlane(upto, 63);
+    };
+    int len, upto, total = scan(0, len, upto);
+    const int first = total;
+    for (int b0 = 64; b0 < p.batch; b0 += 64) {
+        int l, u;
+        total += scan(b0, l, u);
+    }
+    y.share = (max((total + a.shares - 1) / a.shares, kMinShare) + 3) & ~3;
+    int before = 0, sum = first;
     for (int b0 = 0; b0 < p.batch; b0 += 64) {
-        const int b = b0 + lane, len = b < p.batch ? length_of(p, b) : 0;
-        const int n = b >= p.batch ? 0 : len > 0 ? (len - 1) / r.chunk + 1 : 1;
-        int upto = n;
-#pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-            const int y = __shfl_up(upto, s);
-            upto += lane >= s ? y : 0;
-        }
-        const int all = __builtin_amdgcn_readlane(upto, 63);
-        if (BY_RANGE ? x < before + all : x < b0 + 64) {
-            const int l = BY_RANGE ? __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > x)) : x - b0;
-            r.b = b0 + l;
-            r.parts = __builtin_amdgcn_readlane(n, l);
-            r.first = before + __builtin_amdgcn_readlane(upto, l) - r.parts;
-            r.len = __builtin_amdgcn_readlane(len, l);
-            r.part = x - r.first;
+        if (b0) sum = scan(b0, len, upto);
+        if (BY_SHARE ? (int64_t)x * y.share < before + sum : x < b0 + 64) {
+            const int l = BY_SHARE ? __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > x * y.share)) : x - b0;
+            y.b = b0 + l;
+            y.len = __builtin_amdgcn_readlane(len, l);
+            y.before = before + __builtin_amdgcn_readlane(upto, l) - units_of(y.len);
             return true;
         }
-        before += all;
+        before += sum;
     }
     return false;
 }
 
+// Range `part` of those that a sequence is cut into.
+__device__ __forceinline__ Range cut_range(Args &a, int x)
+{
+    Range r;
+    r.b = x / a.parts;
+    const int part = x - r.b * a.parts;
+    r.len = __builtin_amdgcn_readfirstlane(length_of(a.p, r.b));
+    const int chunk = ((r.len + a.parts - 1) / a.parts + 63) & ~63;
+    r.k0 = min(part * chunk, r.len);
+    r.k1 = min(r.k0 + chunk, r.len);
+    r.slot = x;
+    r.whole = a.parts == 1;
+    return r;
+}
+__device__ __forceinline__ Range prefix_range(Args &a, int x)
+{
+    Range r;
+    r.b = 0;
+    r.len = a.p.prefix;
+    r.k0 = x * a.prefix_chunk;
+    r.k1 = min(r.k0 + a.prefix_chunk, r.len);
+    r.slot = x;
+    r.whole = false;
+    return r;
+}
+
 // ---- tiles of keys in LDS ---------------------------------------------------------------------------
 // Kept as sub-blocks of 16 keys, rows of 2 D bytes, without gaps (a direct copy's LDS side is linear).  The 16-byte chunks
-// of a row are permuted among themselves, c -> c ^ swizzle(row), on the global side of the copy, so that 16 rows read at
-// one chunk (K) or at a pair of chunks (V) use all banks evenly.
-template <int D> __device__ __forceinline__ int swizzle(int row) { return D == 128 ? row & 15 : ((row >> 1) & 3) * 2 + ((row >> 3) & 1); }
+// of a row are permuted among themselves, c -> c ^ swizzle(row), on the global side of the copy, so that no two of the lanes
+// that an LDS read serves together meet in a bank: 16 rows at one chunk (K, 16 bytes a lane); V, 32 lanes of 8 bytes: rows
+// 0 .. 7 (and 8 .. 15) at a pair of chunks, or rows 0 .. 3 (4 .. 7, ...) at two pairs, 8 chunks apart (width 64: 2).
+template <int D> __device__ __forceinline__ int swizzle(int row)
+{
+    return D == 128 ? (row << 1 & 14) | (row >> 3 & 1) : (row << 1 & 4) | (row >> 1 & 2) | (row >> 3 & 1);
+}
 
 template <int D> struct SubBlock {
     static constexpr int BYTES = kSub * D * 2;
@@ -129,12 +193,6 @@ template <int D> struct SubBlock {
     }
 };
 
-// the page table is read through the scalar cache, which neither the copies' counter nor their waits know of
-__device__ __forceinline__ int page_id(const int32_t *table, int token, int log2, int last)
-{
-    return ((const __attribute__((address_space(4))) int32_t *)table)[min(token >> log2, last)];
-}
-
 // max over lanes l, l ^ 16, l ^ 32, l ^ 48
 __device__ __forceinline__ float quad_max(float x)
 {
@@ -154,17 +212,19 @@ struct Row {
     int b, i, h;                                         // sequence, new token, query head
     bool stored;                                         // there is such a row
 };
-template <bool PREFIX> __device__ __forceinline__ Row row_of(const Launch &a, int r, int b, int hk)
+template <bool PREFIX> __device__ __forceinline__ Row row_of(int rows, int group, int seqlen, int r, int b, int hk)
 {
-    const PagedParams &p = a.p;
-    const int rr = min(r, a.rows - 1), t = rr / p.group;
+    const int rr = min(r, rows - 1), t = rr / group;
     Row x;
-    x.b = PREFIX ? t / p.seqlen : b;
-    x.i = PREFIX ? t - x.b * p.seqlen : t;
-    x.h = hk * p.group + rr - t * p.group;
-    x.stored = r < a.rows;
+    x.b = PREFIX ? t / seqlen : b;
+    x.i = PREFIX ? t - x.b * seqlen : t;
+    x.h = hk * group + rr - t * group;
+    x.stored = r < rows;
     return x;
 }
+
+// A row's result: the sum of its weights l and their maximum's exponent m give the log-sum-exp.
+__device__ __forceinline__ float natural_lse(float m, float l) { return l > 0.f ? 0.6931471805599453f * (m + __builtin_amdgcn_logf(l)) : -INFINITY; }
 
 // ---- few rows: keys streamed once ---------------------------------------------------------------------
 // A workgroup is NW waves on 16 * NRT rows of one unit and one range of keys.  Every wave takes tiles of 32 keys of its own
@@ -175,38 +235,36 @@ template <bool PREFIX> __device__ __forceinline__ Row row_of(const Launch &a, in
 //   an order of the keys that V's reads share, so P never leaves the registers.
 // Rounded: P to the element type for the second product (its operands have it); l sums the unrounded fp32 values.
 constexpr int kStages = 2;
+constexpr int kWaves = 4;
 
-template <int D, int NW, int NRT, bool F16, bool PREFIX>
-__global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a)
+template <int D, int NRT> struct StreamLds {
+    static constexpr int STAGE = 2 * SubBlock<D>::BYTES;                 // K and V of a tile
+    unsigned char ring[kWaves * kStages * STAGE];
+    float m[kWaves][kSub * NRT], l[kWaves][kSub * NRT];                  // (where the waves' results are joined)
+};
+
+template <int D, int NRT, bool F16, bool PREFIX>
+__device__ __forceinline__ void stream_range(Args &a, const Range r, int hk, int rg, StreamLds<D, NRT> &shared)
 {
     typedef typename Elem<F16>::T el;
     typedef typename Elem<F16>::x8 el8;
+    typedef typename Elem<F16>::x4 el4;
     typedef SubBlock<D> SB;
+    constexpr int NW = kWaves;
+    constexpr int KEYS = kSub;
     constexpr int KI = D / 32;                           // MFMAs of a score tile
     constexpr int DB = D / 16;                           // 16-row blocks of O^T
-    constexpr int STAGE = 4 * SB::BYTES;                 // K of two sub-blocks, V of two
-    constexpr int PER_STAGE = 4 * SB::UNITS;             // copies
+    constexpr int STAGE = StreamLds<D, NRT>::STAGE;
+    constexpr int PER_STAGE = 2 * SB::UNITS;             // copies
     constexpr int OPITCH = D + 4;                        // floats of a row where the waves' results are joined
     static_assert(NW * kSub * OPITCH * 4 <= NW * kStages * STAGE, "joining fits the ring");
-    __shared__ __attribute__((aligned(1024))) unsigned char ring[NW * kStages * STAGE];
-    __shared__ float red_m[NW][kSub * NRT], red_l[NW][kSub * NRT];
 
-    const PagedParams &p = a.p;
+    Params &p = a.p;
+    const bool masked = !PREFIX && p.causal;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hk = blockIdx.x % p.hkv, w = blockIdx.x / p.hkv;
-    const int rg = w % a.groups, x = w / a.groups;
-    Range r;
-    int qn = p.seqlen, k0, k1;
-    if constexpr (PREFIX) {
-        r.b = 0, r.part = x, r.parts = a.parts, r.first = 0, r.len = p.prefix;
-        k0 = x * a.chunk;
-        k1 = min(p.prefix, k0 + a.chunk);
-    } else {
-        if (!find_range<true>(a, x, r)) return;
-        qn = __builtin_amdgcn_readfirstlane(queries_of(p, r.b));
-        k0 = r.part * r.chunk;                           // (part 0 where chunk is the largest number)
-        k1 = (int)min((int64_t)r.len, (int64_t)k0 + r.chunk);
-    }
+    const int qn = PREFIX ? p.seqlen : __builtin_amdgcn_readfirstlane(queries_of(p, r.b));
+    const int k0 = r.k0, rows = PREFIX ? a.prefix_rows : a.rows;
+    int k1 = r.k1;
     const int row0 = rg * kSub * NRT;
     const int n16 = lane & 15, quad = lane >> 4;
     int sees[NRT];                                       // keys below it are visible to this lane's row
@@ -214,11 +272,11 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
 #pragma unroll
     for (int t = 0; t < NRT; ++t) {
         sees[t] = k1;
-        if (!PREFIX && p.causal) sees[t] = min(k1, r.len - qn + row_of<PREFIX>(a, row0 + t * kSub + n16, r.b, hk).i + 1);
+        if (masked) sees[t] = min(k1, r.len - qn + row_of<PREFIX>(rows, p.group, p.seqlen, row0 + t * kSub + n16, r.b, hk).i + 1);
     }
-    if (!PREFIX && p.causal) {
+    if (masked) {
         all_see = min(k1, r.len - qn + row0 / p.group + 1);
-        k1 = min(k1, r.len - qn + min(row0 + kSub * NRT - 1, a.rows - 1) / p.group + 1);      // keys that some row sees
+        k1 = min(k1, r.len - qn + min(row0 + kSub * NRT - 1, rows - 1) / p.group + 1);      // keys that some row sees
     }
 
     const int32_t *table = PREFIX ? p.prefix_table : p.table + r.b * p.tsb;
@@ -226,7 +284,7 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
     el8 q[NRT][KI];
 #pragma unroll
     for (int t = 0; t < NRT; ++t) {
-        const Row y = row_of<PREFIX>(a, row0 + t * kSub + n16, r.b, hk);
+        const Row y = row_of<PREFIX>(rows, p.group, p.seqlen, row0 + t * kSub + n16, r.b, hk);
         const uint16_t *src = p.q + y.b * p.qsb + y.i * p.qsn + y.h * p.qsh + quad * 8;
 #pragma unroll
         for (int i = 0; i < KI; ++i) q[t][i] = *reinterpret_cast<const el8 *>(src + 32 * i);
@@ -234,26 +292,25 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
     uint32_t koff[SB::UNITS], voff[SB::UNITS];
     SB::offsets(koff, lane, p.pages.ksn);
     SB::offsets(voff, lane, p.pages.vsn);
-    const uint32_t mine = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)ring) + wave * kStages * STAGE;
+    const uint32_t mine = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)shared.ring) + wave * kStages * STAGE;
     const uint16_t *const kh = p.k_cache + hk * p.pages.ksh, *const vh = p.v_cache + hk * p.pages.vsh;
 
-    struct Ids { int id[2]; };
-    auto ids_of = [&](int key) {                         // pages of a tile's two sub-blocks
-        Ids y;
-        y.id[0] = page_id(table, key, p.pages.page_log2, last_page);
-        y.id[1] = page_id(table, key + kSub, p.pages.page_log2, last_page);
-        return y;
+    // Pages: lane i holds the page of this wave's tile 64 w + i of window w, read once for 64 tiles (the wait for them is one
+    // for the copies in flight, too).  Through the scalar cache a page would be in the way of every LDS read, whose waits
+    // cannot tell the two apart.
+    constexpr int STEP = KEYS * NW;
+    const int first = k0 + KEYS * wave;
+    int window = 0;
+    auto page_of = [&](int tile) {
+        if ((tile & 63) == 0) window = table[min((first + (tile + lane) * STEP) >> p.pages.page_log2, last_page)];
+        return __builtin_amdgcn_readlane(window, tile & 63);
     };
-    // keys of a sub-block that exist: none where it lies behind the range or its page is none of the cache's
+    // keys of a tile that exist: none where it lies behind the range or its page is none of the cache's
     auto exist = [&](int key, int id) { return __builtin_amdgcn_readfirstlane((unsigned)id < (unsigned)p.pages.n_pages ? min(max(k1 - key, 0), kSub) : 0); };
-    auto request = [&](int key, const Ids &ids, uint32_t at) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int n = exist(key + s * kSub, ids.id[s]);
-            const int64_t id = n > 0 ? ids.id[s] : 0, place = (key + s * kSub) & in_page;
-            SB::copy(kh + id * p.pages.ksp + place * p.pages.ksn, n, p.pages.ksn, koff, at + s * SB::BYTES);
-            SB::copy(vh + id * p.pages.vsp + place * p.pages.vsn, n, p.pages.vsn, voff, at + (2 + s) * SB::BYTES);
-        }
+    auto request = [&](int key, int page, int n, uint32_t at) {
+        const int64_t id = n > 0 ? page : 0, place = key & in_page;
+        SB::copy(kh + id * p.pages.ksp + place * p.pages.ksn, n, p.pages.ksn, koff, at);
+        SB::copy(vh + id * p.pages.vsp + place * p.pages.vsn, n, p.pages.vsn, voff, at + SB::BYTES);
     };
 
     f32x4 o[NRT][DB];
@@ -273,56 +330,47 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
     for (int i = 0; i < KI; ++i) ka[i] = n16 * (D * 2) + (((4 * i + quad) ^ swizzle<D>(n16)) * 16);
     const int vrow = 4 * quad + (n16 >> 2);
 #pragma unroll
-    for (int x = 0; x < DB; ++x) va[x] = vrow * (D * 2) + (((2 * x + ((n16 >> 1) & 1)) ^ swizzle<D>(vrow)) * 16) + (n16 & 1) * 8 + 2 * SB::BYTES;
+    for (int x = 0; x < DB; ++x) va[x] = vrow * (D * 2) + (((2 * x + ((n16 >> 1) & 1)) ^ swizzle<D>(vrow)) * 16) + (n16 & 1) * 8 + SB::BYTES;
 
-    constexpr int STEP = 32 * NW;
-    int key = k0 + 32 * wave;
-    Ids now = ids_of(key), next = ids_of(key + STEP);
     // the queries arrive before the copies are requested: a wait for them would wait for the copies, too
 #pragma unroll
     for (int t = 0; t < NRT; ++t)
 #pragma unroll
         for (int i = 0; i < KI; ++i) asm volatile("" : "+v"(q[t][i]));
-    request(key, now, mine);
-    request(key + STEP, next, mine + STAGE);
-    Ids after = ids_of(key + 2 * STEP);
+    int now, next;                                       // keys of the tile at hand and of the next one that exist
+    {
+        const int page = page_of(0), page2 = page_of(1);
+        now = exist(first, page);
+        next = exist(first + STEP, page2);
+        request(first, page, now, mine);
+        request(first + STEP, page2, next, mine + STAGE);
+    }
     uint32_t at = mine;
-    for (; key < k1; key += STEP) {
+    for (int tile = 0, key = first; key < k1; ++tile, key += STEP) {
         wait_vmcnt<PER_STAGE>();
         asm volatile("" : : : "memory");
-        f32x4 s[NRT][2];
+        f32x4 s[NRT];
 #pragma unroll
-        for (int t = 0; t < NRT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < KI; ++i) {
+            const el8 kk = *LDS_PTR(const el8, at + ka[i]);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int i = 0; i < KI; ++i) {
-                const el8 kk = *LDS_PTR(const el8, at + ka[i] + kb * SB::BYTES);
-#pragma unroll
-                for (int t = 0; t < NRT; ++t) s[t][kb] = mfma32(kk, q[t][i], s[t][kb]);
-            }
-        const int n0 = exist(key, now.id[0]), n1 = exist(key + kSub, now.id[1]);
-        if (n0 + n1 < 32 || key + 32 > all_see) {
+            for (int t = 0; t < NRT; ++t) s[t] = mfma32(kk, q[t][i], i == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t]);
+        }
+        if (now < KEYS || key + KEYS > all_see) {
 #pragma unroll
             for (int t = 0; t < NRT; ++t)
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int y = 4 * quad + e;
-                        if (y >= (kb ? n1 : n0) || key + kb * kSub + y >= sees[t]) s[t][kb][e] = -INFINITY;
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const int y = 4 * quad + e;
+                    if (!((y < now) & (key + y < sees[t]))) s[t][e] = -INFINITY;
+                }
         }
-        el8 pr[NRT];
+        el4 pr[NRT];
 #pragma unroll
         for (int t = 0; t < NRT; ++t) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][kb][e]);
-            mx = fmaxf(m[t], quad_max(mx) * p.scale_log2);
-            if (__builtin_amdgcn_ballot_w64(mx > m[t])) {
+            float mx = quad_max(fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3]))) * p.scale_log2;
+            if (__builtin_amdgcn_ballot_w64(mx > m[t] + kSlack)) {
+                mx = mx > m[t] + kSlack ? mx : m[t];
                 const float f = __builtin_amdgcn_exp2f(m[t] - mx);
                 l[t] *= f;
 #pragma unroll
@@ -330,28 +378,24 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
                 m[t] = mx;
             }
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float y = __builtin_amdgcn_exp2f(fmaf(s[t][kb][e], p.scale_log2, -m[t]));
-                    l[t] += y;
-                    pr[t][4 * kb + e] = (el)y;
-                }
+            for (int e = 0; e < 4; ++e) {
+                const float y = __builtin_amdgcn_exp2f(fmaf(s[t][e], p.scale_log2, -m[t]));
+                l[t] += y;
+                pr[t][e] = (el)y;
+            }
         }
 #pragma unroll
         for (int x = 0; x < DB; ++x) {
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + va[x]));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + va[x] + SB::BYTES));
-            const el8 vv = __builtin_bit_cast(el8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            const s16x4 vv = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, at + va[x]));
 #pragma unroll
-            for (int t = 0; t < NRT; ++t) o[t][x] = mfma32(vv, pr[t], o[t][x]);
+            for (int t = 0; t < NRT; ++t) o[t][x] = mfma16x16(vv, pr[t], o[t][x]);
         }
         __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0): this tile has been read
         asm volatile("" : : : "memory");
-        request(key + 2 * STEP, after, at);
+        const int page = page_of(tile + 2), n = exist(key + 2 * STEP, page);
+        request(key + 2 * STEP, page, n, at);
         now = next;
-        next = after;
-        after = ids_of(key + 3 * STEP);
+        next = n;
         at ^= mine ^ (mine + STAGE);
     }
 
@@ -361,14 +405,16 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
     for (int t = 0; t < NRT; ++t) {
         l[t] = quad_sum(l[t]);
         if (quad == 0) {
-            red_m[wave][t * kSub + n16] = m[t];
-            red_l[wave][t * kSub + n16] = l[t];
+            shared.m[wave][t * kSub + n16] = m[t];
+            shared.l[wave][t * kSub + n16] = l[t];
         }
     }
-    float *const ro = reinterpret_cast<float *>(ring);
+    float *const ro = reinterpret_cast<float *>(shared.ring);
     constexpr int TPR = NW * 64 / kSub, DPT = D / TPR;   // threads of a row, elements of a thread
-    const int jr = threadIdx.x / TPR, jd = threadIdx.x % TPR * DPT;
-    const bool direct = !PREFIX && a.direct && r.parts == 1;
+    const int tid = anew(threadIdx.x), jr = tid / TPR, jd = tid % TPR * DPT;
+    Args &z = arguments();
+    const int end_rows = PREFIX ? z.prefix_rows : z.rows;
+    const bool direct = z.direct && r.whole;
 #pragma unroll
     for (int t = 0; t < NRT; ++t) {
         __syncthreads();
@@ -376,37 +422,69 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
         for (int x = 0; x < DB; ++x) *reinterpret_cast<f32x4 *>(ro + (wave * kSub + n16) * OPITCH + 16 * x + 4 * quad) = o[t][x];
         __syncthreads();
         const int row = row0 + t * kSub + jr;
-        const Row y = row_of<PREFIX>(a, row, r.b, hk);
         float mm = kNone, ll = 0.f, oo[DPT];
 #pragma unroll
-        for (int v = 0; v < NW; ++v) mm = fmaxf(mm, red_m[v][t * kSub + jr]);
+        for (int v = 0; v < NW; ++v) mm = fmaxf(mm, shared.m[v][t * kSub + jr]);
 #pragma unroll
         for (int d = 0; d < DPT; ++d) oo[d] = 0.f;
 #pragma unroll
         for (int v = 0; v < NW; ++v) {
-            const float f = __builtin_amdgcn_exp2f(red_m[v][t * kSub + jr] - mm);
-            ll = fmaf(f, red_l[v][t * kSub + jr], ll);
+            const float f = __builtin_amdgcn_exp2f(shared.m[v][t * kSub + jr] - mm);
+            ll = fmaf(f, shared.l[v][t * kSub + jr], ll);
 #pragma unroll
             for (int d = 0; d < DPT; ++d) oo[d] = fmaf(f, ro[(v * kSub + jr) * OPITCH + jd + d], oo[d]);
         }
+        const Row y = row_of<PREFIX>(end_rows, z.p.group, z.p.seqlen, row, r.b, hk);
         if (!y.stored) continue;
         if (direct) {
             if (y.i >= qn) continue;
             const float f = ll > 0.f ? 1.f / ll : 0.f;   // (a row that sees nothing: 0)
-            uint16_t *dst = p.out + y.b * p.osb + y.i * p.osn + y.h * p.osh + jd;
+            uint16_t *dst = z.p.out + y.b * z.p.osb + y.i * z.p.osn + y.h * z.p.osh + jd;
             typedef el elx __attribute__((ext_vector_type(DPT)));
-            elx z;
+            elx w;
 #pragma unroll
-            for (int d = 0; d < DPT; ++d) z[d] = (el)(oo[d] * f);
-            *reinterpret_cast<elx *>(dst) = z;
-            if (p.lse && jd == 0) p.lse[((int64_t)y.b * p.seqlen + y.i) * p.hq + y.h] = ll > 0.f ? 0.6931471805599453f * (mm + __builtin_amdgcn_logf(ll)) : -INFINITY;
+            for (int d = 0; d < DPT; ++d) w[d] = (el)(oo[d] * f);
+            *reinterpret_cast<elx *>(dst) = w;
+            if (z.p.lse && jd == 0) z.p.lse[((int64_t)y.b * z.p.seqlen + y.i) * z.p.hq + y.h] = natural_lse(mm, ll);
         } else {
-            const int64_t slot = ((int64_t)(PREFIX ? x : r.first + r.part) * p.hkv + hk) * a.rows + row;
-            float *dst = (PREFIX ? a.prefix_o : a.own_o) + slot * D + jd;
+            const int64_t at = ((int64_t)r.slot * z.p.hkv + hk) * end_rows + row;
+            float *dst = (PREFIX ? z.prefix_o : z.own_o) + at * D + jd;
 #pragma unroll
             for (int d = 0; d < DPT; d += 4) *reinterpret_cast<f32x4 *>(dst + d) = f32x4{oo[d], oo[d + 1], oo[d + 2], oo[d + 3]};
-            if (jd == 0) (PREFIX ? a.prefix_ml : a.own_ml)[slot] = make_float2(mm, ll);
+            if (jd == 0) (PREFIX ? z.prefix_ml : z.own_ml)[at] = make_float2(mm, ll);
         }
+    }
+}
+
+// The sequences' own tokens: those of workgroup x.
+template <int D, int NRT, bool F16>
+__device__ __forceinline__ void stream_own(Args &a, int hk, int x, int rg, StreamLds<D, NRT> &shared)
+{
+    Range r;
+    Share y;
+    int from = 0, to = 0;
+    if (a.shares) {
+        if (!even_share<true>(a, x, y)) return;
+        from = x * y.share;
+        to = from + y.share;
+    }
+    while (true) {
+        if (a.shares) {
+            const int units = units_of(y.len);
+            r.b = y.b;
+            r.len = y.len;
+            r.k0 = max(from - y.before, 0) * kSub;
+            r.k1 = min(r.len, (to - y.before) * kSub);
+            r.slot = x + y.b;
+            r.whole = from <= y.before && y.before + units <= to;
+            y.before += units;
+        } else {
+            r = cut_range(a, x);
+        }
+        stream_range<D, NRT, F16, false>(a, r, hk, rg, shared);
+        if (!a.shares || y.before >= to || ++y.b >= a.p.batch) return;
+        y.len = __builtin_amdgcn_readfirstlane(length_of(a.p, y.b));
+        __syncthreads();                                 // (the ring is free again)
     }
 }
 
@@ -419,8 +497,12 @@ __global__ void __launch_bounds__(NW * 64, 1) paged_stream_kernel(const Launch a
 // Two workgroups on a CU hide each other's barriers.
 constexpr int kTileRows = 128, kTileKeys = 64;
 
+template <int D> struct TileLds {
+    unsigned char ring[16 * SubBlock<D>::BYTES];
+};
+
 template <int D, bool F16, bool PREFIX>
-__global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
+__device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int rg, TileLds<D> &shared)
 {
     typedef typename Elem<F16>::T el;
     typedef typename Elem<F16>::x8 el8;
@@ -430,33 +512,23 @@ __global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
     constexpr int PD = 4;                                // operand reads run that many MFMAs ahead
     constexpr int SLOT = 4 * SB::BYTES;
     constexpr uint32_t K0 = 0, V0 = 2 * SLOT;
-    __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * SLOT];
 
-    const PagedParams &p = a.p;
+    Params &p = a.p;
+    const bool causal = !PREFIX && p.causal;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hk = blockIdx.x % p.hkv, w = blockIdx.x / p.hkv;
-    const int rg = a.groups - 1 - w % a.groups, x = w / a.groups;      // later rows see more keys: first
-    Range r;
-    int qn = p.seqlen, k0, k1;
-    if constexpr (PREFIX) {
-        r.b = 0, r.part = x, r.parts = a.parts, r.first = 0, r.len = p.prefix;
-        k0 = x * a.chunk;
-        k1 = min(p.prefix, k0 + a.chunk);
-    } else {
-        if (!find_range<true>(a, x, r)) return;
-        qn = __builtin_amdgcn_readfirstlane(queries_of(p, r.b));
-        k0 = r.part * r.chunk;
-        k1 = (int)min((int64_t)r.len, (int64_t)k0 + r.chunk);
-    }
+    const int qn = PREFIX ? p.seqlen : __builtin_amdgcn_readfirstlane(queries_of(p, r.b));
+    const int k0 = r.k0, rows = PREFIX ? a.prefix_rows : a.rows;
+    int k1 = r.k1;
     const int row0 = rg * kTileRows;
-    if (!PREFIX && row0 >= qn * p.group && a.direct && r.parts == 1) return;         // (no row to store)
+    const bool direct = a.direct && r.whole;
+    if (direct && row0 >= qn * p.group) return;          // (no row to store)
     const int l32 = lane & 31, hh = lane >> 5;
-    const Row mine = row_of<PREFIX>(a, row0 + wave * 32 + l32, r.b, hk);
+    const Row mine = row_of<PREFIX>(rows, p.group, p.seqlen, row0 + wave * 32 + l32, r.b, hk);
     int sees = k1, all_see = k1;
-    if (!PREFIX && p.causal) {
+    if (causal) {
         sees = min(k1, r.len - qn + mine.i + 1);
         all_see = min(k1, r.len - qn + (row0 + wave * 32) / p.group + 1);             // (of this wave's rows)
-        k1 = min(k1, r.len - qn + min(row0 + kTileRows - 1, a.rows - 1) / p.group + 1);
+        k1 = min(k1, r.len - qn + min(row0 + kTileRows - 1, rows - 1) / p.group + 1);
     }
     const int n_tiles = max(0, (k1 - k0 + kTileKeys - 1) / kTileKeys);
 
@@ -471,28 +543,23 @@ __global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
     uint32_t koff[SB::UNITS], voff[SB::UNITS];
     SB::offsets(koff, lane, p.pages.ksn);
     SB::offsets(voff, lane, p.pages.vsn);
-    const uint32_t lds = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)ring);
+    const uint32_t lds = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)shared.ring);
     const uint16_t *const kh = p.k_cache + hk * p.pages.ksh, *const vh = p.v_cache + hk * p.pages.vsh;
 
-    // the pages of a tile's sub-blocks, and of this wave's
-    struct Tile { int id[4], mine; };
-    auto tile_of = [&](int t) {
-        Tile y;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) y.id[s] = page_id(table, k0 + t * kTileKeys + s * kSub, p.pages.page_log2, last_page);
-        y.mine = page_id(table, k0 + t * kTileKeys + wave * kSub, p.pages.page_log2, last_page);
-        return y;
-    };
-    auto in_cache = [&](int id) { return (unsigned)id < (unsigned)p.pages.n_pages; };
+    // Pages of a tile's sub-blocks, one to a lane (of four).  They arrive with the copies that are requested next to them; through
+    // the scalar cache they would be in the way of every LDS read, whose waits cannot tell the two apart.
+    auto tile_of = [&](int t) { return table[min((k0 + t * kTileKeys + (lane & 3) * kSub) >> p.pages.page_log2, last_page)]; };
+    // which of the four are pages of the cache
+    auto in_cache = [&](int pages) { return (uint32_t)__builtin_amdgcn_ballot_w64((unsigned)pages < (unsigned)p.pages.n_pages) & 15u; };
     struct Source { i32x4 rsrc; uint32_t dst; };
-    auto source = [&](const uint16_t *base, int64_t sp, int64_t sn, int t, const Tile &y, uint32_t slot) {
-        const int key = k0 + t * kTileKeys + wave * kSub;
-        const int n = __builtin_amdgcn_readfirstlane(in_cache(y.mine) ? min(max(k1 - key, 0), kSub) : 0);
-        const int64_t id = n > 0 ? y.mine : 0;
+    auto source = [&](const uint16_t *base, int64_t sp, int64_t sn, int t, int pages, uint32_t slot) {
+        const int key = k0 + t * kTileKeys + wave * kSub, page = __builtin_amdgcn_readlane(pages, wave);
+        const int n = __builtin_amdgcn_readfirstlane((unsigned)page < (unsigned)p.pages.n_pages ? min(max(k1 - key, 0), kSub) : 0);
+        const int64_t id = n > 0 ? page : 0;
         return Source{SB::descriptor(base + id * sp + (key & in_page) * sn, n, sn), (uint32_t)__builtin_amdgcn_readfirstlane(lds + slot + wave * SB::BYTES)};
     };
-    auto k_source = [&](int t, const Tile &y, uint32_t slot) { return source(kh, p.pages.ksp, p.pages.ksn, t, y, K0 + slot); };
-    auto v_source = [&](int t, const Tile &y, uint32_t slot) { return source(vh, p.pages.vsp, p.pages.vsn, t, y, V0 + slot); };
+    auto k_source = [&](int t, int pages, uint32_t slot) { return source(kh, p.pages.ksp, p.pages.ksn, t, pages, K0 + slot); };
+    auto v_source = [&](int t, int pages, uint32_t slot) { return source(vh, p.pages.vsp, p.pages.vsn, t, pages, V0 + slot); };
 
     // operand addresses.  K: row 32 kb + l32, elements 16 s + 8 hh .. + 7.  V: keys 16 u + 4 hh + 8 half + (L >> 2), 4 elements
     // from G16 * g16 + X * x + 4 (L & 3) on, transposed within 16 lanes: operand row 16 g16 + L of block x is that element of O
@@ -526,22 +593,21 @@ __global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
     uint64_t grown = 0;                                  // lanes whose row's maximum has grown with the next tile
 
     struct Scores { f32x16 s[2]; };
-    auto masked = [&](Scores &z, int t, const Tile &y) {
+    auto masked = [&](Scores &z, int t, int pages) {
         const int key = k0 + t * kTileKeys;
-        bool there[4];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) there[s] = in_cache(y.id[s]);
-        if (there[0] & there[1] & there[2] & there[3] & (key + kTileKeys <= all_see)) return;
+        const uint32_t there = in_cache(pages);
+        if ((there == 15u) & (key + kTileKeys <= all_see)) return;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int y = 32 * kb + 8 * (e >> 2) + 4 * hh + (e & 3);
-                z.s[kb][e] = there[2 * kb + (e >> 3)] & (key + y < sees) ? z.s[kb][e] : -INFINITY;
+                if (!((there >> (2 * kb + (e >> 3)) & 1u) & (key + y < sees))) z.s[kb][e] = -INFINITY;
             }
     };
     auto new_max = [&](float mx) {                       // of the raw scores, in both lanes of the row
-        const float y = fmaxf(m, mx * p.scale_log2);
+        mx *= p.scale_log2;
+        const float y = mx > m + kSlack ? mx : m;
         grown = __builtin_amdgcn_ballot_w64(y > m);
         alpha = __builtin_amdgcn_exp2f(m - y);
         l *= alpha;
@@ -550,16 +616,19 @@ __global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
     auto prob = [&](const Scores &z, int n) { return __builtin_amdgcn_exp2f(fmaf(z.s[n >> 4][n & 15], p.scale_log2, -m)); };
 
     el8 kpre[PD];
-    Tile t1, t2, t3;                                     // pages of tiles j + 1, j + 2, j + 3
+    int t1, t2, t3;                                      // pages of tiles j + 1, j + 2, j + 3
     // Stage j on the slots of its parity: cur -> P, next <- scores of tile j + 1, if there is one.
     auto stage = [&](auto parity, auto last, Scores &cur, Scores &next, int j) {
         constexpr uint32_t S0 = decltype(parity)::value * SLOT, S1 = SLOT - S0;      // slots of tile j and j + 1
         constexpr bool LAST = decltype(last)::value;
         el8 pr[4];
-        float ex[EPM], sum[2] = {0.f, 0.f};
-        auto pack = [&](int n) {
-#pragma unroll
-            for (int t = 0; t < EPM; ++t) pr[(n * EPM + t) >> 3][(n * EPM + t) & 7] = (el)ex[t];
+        float ex[32], sum[2] = {0.f, 0.f};
+        auto round_and_sum = [&](auto slot) {            // those of the slot before: nothing waits for a transcendental just issued
+            static_range<decltype(slot)::value * EPM, (decltype(slot)::value + 1) * EPM>([&](auto t) {
+                pr[t >> 3][t & 7] = (el)ex[t];
+                sum[t & 1] += ex[t];
+            });
+            asm volatile("" : "+v"(sum[0]), "+v"(sum[1]));           // (else the sums are put off, with all they add up kept in registers)
         };
         if constexpr (!LAST) {
 #pragma unroll
@@ -567,33 +636,26 @@ __global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) next.s[kb][e] = 0.f;
         }
+        // (the exponentials stay between these MFMAs: left alone, the compiler moves every other stage's up into the stage
+        // before, whose MFMAs have work enough beside them)
+        asm volatile("" : "+v"(cur.s[0]), "+v"(cur.s[1]));
         el8 ops[NQK + PD];
 #pragma unroll
         for (int n = 0; n < PD; ++n) ops[n] = kpre[n];
-#pragma unroll
-        for (int n = 0; n < NQK; ++n) {
+        static_for<NQK>([&](auto nc) {
+            constexpr int n = decltype(nc)::value;
             if constexpr (!LAST) {
-                if (n + PD < NQK) ops[n + PD] = k_operand(n + PD, S1);
+                if constexpr (n + PD < NQK) ops[n + PD] = k_operand(n + PD, S1);
                 next.s[n & 1] = mfma16(ops[n], q[n >> 1], next.s[n & 1]);
             }
-            float nx[EPM];
-#pragma unroll
-            for (int t = 0; t < EPM; ++t) nx[t] = prob(cur, n * EPM + t);
-            if (n > 0) pack(n - 1);
-#pragma unroll
-            for (int t = 0; t < EPM; ++t) {
-                ex[t] = nx[t];
-                sum[t & 1] += nx[t];
-            }
+            static_range<n * EPM, (n + 1) * EPM>([&](auto t) { ex[t] = prob(cur, t); });
+            if constexpr (n > 0) round_and_sum(std::integral_constant<int, n - 1>{});
             __builtin_amdgcn_sched_barrier(0);
-        }
-        pack(NQK - 1);
+        });
+        round_and_sum(std::integral_constant<int, NQK - 1>{});
         l += sum[0] + sum[1];
-        Tile t4;
-        if constexpr (!LAST) {
-            masked(next, j + 1, t1);
-            t4 = tile_of(j + 4);
-        }
+        asm volatile("" : "+v"(pr[0]), "+v"(pr[1]), "+v"(pr[2]), "+v"(pr[3]), "+v"(l));
+        if constexpr (!LAST) masked(next, j + 1, t1);
         wait_vmcnt<0>();
         wg_barrier();
         __builtin_amdgcn_sched_barrier(0);
@@ -613,7 +675,7 @@ __global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
             vs = v_source(j + 1, t1, S1);
             t1 = t2;
             t2 = t3;
-            t3 = t4;
+            t3 = tile_of(j + 4);
         }
         float mx = -INFINITY;
         static_for<NPV>([&](auto nc) {
@@ -643,7 +705,7 @@ __global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
     };
 
     if (n_tiles > 0) {
-        const Tile t0 = tile_of(0);
+        const int t0 = tile_of(0);
         t1 = tile_of(1);
         t2 = tile_of(2);
         t3 = tile_of(3);
@@ -686,10 +748,11 @@ __global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
     // ---- results, through the LDS so that rows are written in whole lines ---------------------------------------
     wg_barrier();
     l += __shfl_xor(l, 32);
-    const bool direct = !PREFIX && a.direct && r.parts == 1;
+    Args &z = arguments();
+    const int end_rows = PREFIX ? z.prefix_rows : z.rows;
     const float f = !direct ? 1.f : l > 0.f ? 1.f / l : 0.f;
     constexpr int CH = D / 4;                            // 16-byte chunks of a row of 32-bit results
-    float *const ro = reinterpret_cast<float *>(ring) + wave * 32 * D;
+    float *const ro = reinterpret_cast<float *>(shared.ring) + wave * 32 * D;
 #pragma unroll
     for (int y = 0; y < DB; ++y)
 #pragma unroll
@@ -698,161 +761,237 @@ __global__ void __launch_bounds__(256, 2) paged_tile_kernel(const Launch a)
             *reinterpret_cast<f32x4 *>(ro + l32 * D + (((d >> 2) ^ (l32 % CH)) << 2)) =
                 f32x4{o[y][4 * c] * f, o[y][4 * c + 1] * f, o[y][4 * c + 2] * f, o[y][4 * c + 3] * f};
         }
-    if (hh == 0) {
-        const int row = row0 + wave * 32 + l32;
+    const int at_lane = anew(lane);
+    if (at_lane < 32) {
+        const int row = row0 + wave * 32 + at_lane;
+        const Row y = row_of<PREFIX>(end_rows, z.p.group, z.p.seqlen, row, r.b, hk);
         if (direct) {
-            if (p.lse && mine.stored && mine.i < qn)
-                p.lse[((int64_t)mine.b * p.seqlen + mine.i) * p.hq + mine.h] = l > 0.f ? 0.6931471805599453f * (m + __builtin_amdgcn_logf(l)) : -INFINITY;
-        } else if (mine.stored)
-            (PREFIX ? a.prefix_ml : a.own_ml)[((int64_t)(PREFIX ? x : r.first + r.part) * p.hkv + hk) * a.rows + row] = make_float2(m, l);
+            if (z.p.lse && y.stored && y.i < qn) z.p.lse[((int64_t)y.b * z.p.seqlen + y.i) * z.p.hq + y.h] = natural_lse(m, l);
+        } else if (y.stored)
+            (PREFIX ? z.prefix_ml : z.own_ml)[((int64_t)r.slot * z.p.hkv + hk) * end_rows + row] = make_float2(m, l);
     }
     constexpr int AT_ONCE = 64 / CH;                     // rows
-    for (int y = lane / CH; y < 32; y += AT_ONCE) {
-        const int row = row0 + wave * 32 + y, c = lane % CH;
-        const Row z = row_of<PREFIX>(a, row, r.b, hk);
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(ro + y * D + ((c ^ (y % CH)) << 2));
-        if (!z.stored) continue;
+    for (int n = at_lane / CH; n < 32; n += AT_ONCE) {
+        const int row = row0 + wave * 32 + n, c = at_lane % CH;
+        const Row y = row_of<PREFIX>(end_rows, z.p.group, z.p.seqlen, row, r.b, hk);
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(ro + n * D + ((c ^ (n % CH)) << 2));
+        if (!y.stored) continue;
         if (direct) {
-            if (z.i >= qn) continue;
+            if (y.i >= qn) continue;
             typedef el el4 __attribute__((ext_vector_type(4)));
-            *reinterpret_cast<el4 *>(p.out + z.b * p.osb + z.i * p.osn + z.h * p.osh + 4 * c) = el4{(el)v[0], (el)v[1], (el)v[2], (el)v[3]};
+            *reinterpret_cast<el4 *>(z.p.out + y.b * z.p.osb + y.i * z.p.osn + y.h * z.p.osh + 4 * c) = el4{(el)v[0], (el)v[1], (el)v[2], (el)v[3]};
         } else {
-            float *dst = (PREFIX ? a.prefix_o : a.own_o) + (((int64_t)(PREFIX ? x : r.first + r.part) * p.hkv + hk) * a.rows + row) * D;
+            float *dst = (PREFIX ? z.prefix_o : z.own_o) + (((int64_t)r.slot * z.p.hkv + hk) * end_rows + row) * D;
             *reinterpret_cast<f32x4 *>(dst + 4 * c) = v;
         }
     }
 }
 
-// ---- ranges joined --------------------------------------------------------------------------------------
-// A workgroup is one row of one query head: its waves take the ranges in turn, a lane D / 64 elements.
-template <int D, bool F16>
-__global__ void __launch_bounds__(256) paged_join_kernel(const Launch a, const int prefix_rows, const int own_rows)
+// ---- the kernels ------------------------------------------------------------------------------------------
+// One launch for the prefix and few rows of own tokens.  Workgroups of a KV head lie hkv apart, so that with 8 of them
+// (or a multiple) all that read one head's keys share an XCD's L2.
+struct Work {
+    bool prefix;
+    int hk, x, rg;
+};
+__device__ __forceinline__ Work work_of(Args &a)
 {
+    Work w;
+    w.hk = blockIdx.x % a.p.hkv;
+    int v = blockIdx.x / a.p.hkv;
+    const int n = a.prefix_parts * a.prefix_groups;
+    w.prefix = v < n;
+    if (!w.prefix) v -= n;
+    const int groups = w.prefix ? a.prefix_groups : a.groups;
+    w.x = v / groups;
+    w.rg = groups - 1 - (v - w.x * groups);              // (later rows see more keys: first)
+    return w;
+}
+
+template <int D, int NRT, bool F16, bool TILED_PREFIX>
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_stream_kernel(const Launch)
+{
+    __shared__ __attribute__((aligned(1024))) union { StreamLds<D, NRT> stream; TileLds<D> tile; } shared;
+    const Work w = work_of(arguments());
+    if (w.prefix) {
+        Args &a = arguments();
+        const Range r = prefix_range(a, w.x);
+        if constexpr (TILED_PREFIX) tile_range<D, F16, true>(a, r, w.hk, w.rg, shared.tile);
+        else stream_range<D, NRT, F16, true>(a, r, w.hk, w.rg, shared.stream);
+    } else {
+        stream_own<D, NRT, F16>(arguments(), w.hk, w.x, w.rg, shared.stream);
+    }
+}
+
+template <int D, bool F16, bool PREFIX>
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_tile_kernel(const Launch)
+{
+    Args &a = arguments();
+    __shared__ __attribute__((aligned(1024))) TileLds<D> shared;
+    const int hk = blockIdx.x % a.p.hkv, v = blockIdx.x / a.p.hkv, groups = PREFIX ? a.prefix_groups : a.groups;
+    const int x = v / groups, rg = groups - 1 - (v - x * groups);          // (later rows see more keys: first)
+    tile_range<D, F16, PREFIX>(a, PREFIX ? prefix_range(a, x) : cut_range(a, x), hk, rg, shared);
+}
+
+// Ranges joined: WPR waves to a row of one query head, which take its ranges in turn; a lane has D / 64 elements.
+template <int D, bool F16, int WPR>
+__global__ void __launch_bounds__(256) paged_join_kernel(const Launch)
+{
+    Args &a = arguments();
     typedef typename Elem<F16>::T el;
-    constexpr int E = D / 64;
+    constexpr int E = D / 64, ROWS = 4 / WPR;
     typedef float fx __attribute__((ext_vector_type(E)));
     typedef el elx __attribute__((ext_vector_type(E)));
     __shared__ float red[4][D + 2];
-    const PagedParams &p = a.p;
+    Params &p = a.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h = blockIdx.x % p.hq, t = blockIdx.x / p.hq, i = t % p.seqlen, b = t / p.seqlen;
+    const int id = blockIdx.x * ROWS + (WPR == 4 ? 0 : wave), sub = WPR == 4 ? wave : 0;
+    if (id >= p.batch * p.seqlen * p.hq) return;
+    const int t = id / p.hq, h = id - t * p.hq, b = t / p.seqlen, i = t - b * p.seqlen;
     if (i >= __builtin_amdgcn_readfirstlane(queries_of(p, b))) return;
-    Range r;
-    find_range<false>(a, b, r);
-    if (a.direct && r.parts == 1) return;                // written already
+    int slot = b * a.parts, own = a.parts;               // the sequence's ranges
+    if (a.shares) {
+        Share y;
+        even_share<false>(a, b, y);
+        const int w0 = y.before / y.share;
+        own = (y.before + units_of(y.len) - 1) / y.share - w0 + 1;
+        slot = w0 + b;
+    }
+    if (a.direct && own == 1) return;                    // written already
     const int hk = h / p.group, g = h - hk * p.group;
-    const int64_t own_row = (int64_t)i * p.group + g, prefix_row = ((int64_t)b * p.seqlen + i) * p.group + g;
-    const int n = a.parts + r.parts;
+    const int64_t own_at = ((int64_t)slot * p.hkv + hk) * a.rows + i * p.group + g;
+    const int64_t prefix_at = (int64_t)hk * a.prefix_rows + ((int64_t)b * p.seqlen + i) * p.group + g;
+    const int64_t own_step = (int64_t)p.hkv * a.rows, prefix_step = (int64_t)p.hkv * a.prefix_rows;
+    const int n = a.prefix_parts + own;
     float m = kNone, l = 0.f;
     fx o;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int y = wave; y < n; y += 4) {
-        const bool pre = y < a.parts;
-        const int64_t slot = pre ? ((int64_t)y * p.hkv + hk) * prefix_rows + prefix_row : ((int64_t)(r.first + y - a.parts) * p.hkv + hk) * own_rows + own_row;
-        const float2 ml = (pre ? a.prefix_ml : a.own_ml)[slot];
-        const fx v = *reinterpret_cast<const fx *>((pre ? a.prefix_o : a.own_o) + slot * D + lane * E);
-        const float mm = fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - mm), f2 = __builtin_amdgcn_exp2f(ml.x - mm);
-        l = l * f + ml.y * f2;
+    constexpr int AT_ONCE = 4;
+    for (int y0 = sub; y0 < n; y0 += AT_ONCE * WPR) {
+        float2 ml[AT_ONCE];
+        fx v[AT_ONCE];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f + v[e] * f2;
+        for (int c = 0; c < AT_ONCE; ++c) {
+            const int y = min(y0 + c * WPR, n - 1);
+            const bool pre = y < a.prefix_parts;
+            const int64_t at = pre ? prefix_at + y * prefix_step : own_at + (y - a.prefix_parts) * own_step;
+            ml[c] = (pre ? a.prefix_ml : a.own_ml)[at];
+            if (y0 + c * WPR >= n) ml[c] = make_float2(kNone, 0.f);
+            v[c] = *reinterpret_cast<const fx *>((pre ? a.prefix_o : a.own_o) + at * D + lane * E);
+        }
+        float mm = m;
+#pragma unroll
+        for (int c = 0; c < AT_ONCE; ++c) mm = fmaxf(mm, ml[c].x);
+        const float f = __builtin_amdgcn_exp2f(m - mm);
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= f;
+#pragma unroll
+        for (int c = 0; c < AT_ONCE; ++c) {
+            // (a repeated last range counts for nothing)
+            const float w = y0 + c * WPR < n ? __builtin_amdgcn_exp2f(ml[c].x - mm) : 0.f;
+            l = fmaf(ml[c].y, w, l);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(v[c][e], w, o[e]);
+        }
         m = mm;
     }
-    red[wave][D] = m;
-    red[wave][D + 1] = l;
+    if constexpr (WPR == 4) {
+        red[wave][D] = m;
+        red[wave][D + 1] = l;
 #pragma unroll
-    for (int e = 0; e < E; ++e) red[wave][lane * E + e] = o[e];
-    __syncthreads();
-    if (wave != 0) return;
-    for (int y = 1; y < 4; ++y) {
-        const float my = red[y][D], mm = fmaxf(m, my), f = __builtin_amdgcn_exp2f(m - mm), f2 = __builtin_amdgcn_exp2f(my - mm);
-        l = l * f + red[y][D + 1] * f2;
+        for (int e = 0; e < E; ++e) red[wave][lane * E + e] = o[e];
+        __syncthreads();
+        if (wave != 0) return;
+        for (int y = 1; y < 4; ++y) {
+            const float my = red[y][D], mm = fmaxf(m, my), f = __builtin_amdgcn_exp2f(m - mm), f2 = __builtin_amdgcn_exp2f(my - mm);
+            l = l * f + red[y][D + 1] * f2;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f + red[y][lane * E + e] * f2;
-        m = mm;
+            for (int e = 0; e < E; ++e) o[e] = o[e] * f + red[y][lane * E + e] * f2;
+            m = mm;
+        }
     }
     const float f = l > 0.f ? 1.f / l : 0.f;
     elx z;
 #pragma unroll
     for (int e = 0; e < E; ++e) z[e] = (el)(o[e] * f);
     *reinterpret_cast<elx *>(p.out + b * p.osb + i * p.osn + h * p.osh + lane * E) = z;
-    if (p.lse && lane == 0) p.lse[((int64_t)b * p.seqlen + i) * p.hq + h] = l > 0.f ? 0.6931471805599453f * (m + __builtin_amdgcn_logf(l)) : -INFINITY;
+    if (p.lse && lane == 0) p.lse[((int64_t)b * p.seqlen + i) * p.hq + h] = natural_lse(m, l);
 }
 
 // ---- launch -----------------------------------------------------------------------------------------------
-constexpr int kWaves = 4;
-constexpr int kPlaces = 256;         // workgroups of the streaming kernel that the chip holds; twice as many of the other
-constexpr int kFewRows = 64;         // up to that many rows of a unit are streamed
-
+constexpr int kCus = 256;
+constexpr int kFewRows = 32;         // up to that many rows of a unit are streamed
 static int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
+static int row_groups(int rows) { return rows <= kFewRows ? 1 : (rows + kTileRows - 1) / kTileRows; }
 
-struct Plan {
-    Launch own, prefix;
-    int64_t bytes;                   // of workspace
-};
-
-static Plan plan_of(const PagedParams &p, int head_dim)
+// How the work is cut up; returns the bytes of workspace.
+static int64_t plan(Launch &a, int head_dim)
 {
-    Plan y;
-    Launch a = {};
-    a.p = p;
+    const PagedParams &p = a.p;
     a.rows = p.seqlen * p.group;
-    a.groups = a.rows <= kFewRows ? 1 : (a.rows + kTileRows - 1) / kTileRows;
-    const int64_t items = (int64_t)p.batch * p.hkv * a.groups;
-    const int places = a.rows <= kFewRows ? 4 * kPlaces : 2 * kPlaces;
-    a.extra = p.max_len <= 256 || items >= places ? 0 : (int)std::max<int64_t>(1, places / (p.hkv * a.groups));
+    a.groups = row_groups(a.rows);
     a.direct = p.prefix == 0;
-    y.own = a;
-    y.bytes = 0;
-    if (a.extra || !a.direct) {
-        const int64_t rows = (int64_t)(p.batch + a.extra) * p.hkv * a.rows;
-        y.bytes += up256(rows * head_dim * 4) + up256(rows * 8);
+    const int64_t side = (int64_t)p.hkv * a.groups, items = p.batch * side;
+    a.parts = 1;
+    a.shares = 0;
+    if (p.max_len > 256) {
+        if (a.rows <= kFewRows) {
+            if (items < 4 * kCus) a.shares = (int)std::max<int64_t>(1, kCus / side);
+        } else {
+            a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCus / items, p.max_len / 256));
+        }
     }
+    a.own_slots = a.shares ? a.shares + p.batch : p.batch * a.parts;
     if (p.prefix) {
-        Launch &z = y.prefix;
-        z = a;
-        z.rows = p.batch * a.rows;
-        z.groups = z.rows <= kFewRows ? 1 : (z.rows + kTileRows - 1) / kTileRows;
-        const int want = (int)std::max<int64_t>(1, (z.rows <= kFewRows ? 4 : 2) * kPlaces / ((int64_t)p.hkv * z.groups));
-        z.chunk = std::max(128, (int)(((int64_t)p.prefix + want - 1) / want + 127) / 128 * 128);
-        z.parts = (p.prefix + z.chunk - 1) / z.chunk;
-        y.own.parts = z.parts;
-        const int64_t rows = (int64_t)z.parts * p.hkv * z.rows;
-        y.bytes += up256(rows * head_dim * 4) + up256(rows * 8);
+        a.prefix_rows = p.batch * a.rows;
+        a.prefix_groups = row_groups(a.prefix_rows);
+        const int64_t units = (int64_t)p.hkv * a.prefix_groups;
+        const int64_t want = std::max<int64_t>(1, (units <= kCus / 4 ? 1 : 2) * kCus / units);
+        a.prefix_chunk = std::max(128, (int)((p.prefix + want - 1) / want + 63) / 64 * 64);
+        a.prefix_parts = (p.prefix + a.prefix_chunk - 1) / a.prefix_chunk;
     }
+    const bool joined = a.shares || a.parts > 1 || p.prefix;
+    const int64_t own = joined ? (int64_t)a.own_slots * p.hkv * a.rows : 0, prefix = (int64_t)a.prefix_parts * p.hkv * a.prefix_rows;
     unsigned char *at = p.workspace;
-    if (a.extra || !a.direct) {
-        const int64_t rows = (int64_t)(p.batch + a.extra) * p.hkv * a.rows;
-        y.own.own_o = reinterpret_cast<float *>(at);
-        y.own.own_ml = reinterpret_cast<float2 *>(at + up256(rows * head_dim * 4));
-        at += up256(rows * head_dim * 4) + up256(rows * 8);
-    }
-    if (p.prefix) {
-        const int64_t rows = (int64_t)y.prefix.parts * p.hkv * y.prefix.rows;
-        y.own.prefix_o = y.prefix.prefix_o = reinterpret_cast<float *>(at);
-        y.own.prefix_ml = y.prefix.prefix_ml = reinterpret_cast<float2 *>(at + up256(rows * head_dim * 4));
-    }
-    return y;
+    a.own_o = reinterpret_cast<float *>(at);
+    a.own_ml = reinterpret_cast<float2 *>(at += up256(own * head_dim * 4));
+    a.prefix_o = reinterpret_cast<float *>(at += up256(own * 8));
+    a.prefix_ml = reinterpret_cast<float2 *>(at += up256(prefix * head_dim * 4));
+    return at + up256(prefix * 8) - p.workspace;
 }
 
-size_t paged_workspace_bytes(const PagedParams &p, int head_dim) { return (size_t)plan_of(p, head_dim).bytes; }
-
-template <int D, bool F16, bool PREFIX> static void attend(const Launch &a, int64_t ranges, hipStream_t stream)
+size_t paged_workspace_bytes(const PagedParams &p, int head_dim)
 {
-    const unsigned grid = (unsigned)(ranges * a.p.hkv * a.groups);
-    if (a.rows <= 16) paged_stream_kernel<D, kWaves, 1, F16, PREFIX><<<grid, kWaves * 64, 0, stream>>>(a);
-    else if (a.rows <= 32) paged_stream_kernel<D, kWaves, 2, F16, PREFIX><<<grid, kWaves * 64, 0, stream>>>(a);
-    else if (a.rows <= kFewRows) paged_stream_kernel<D, kWaves, 4, F16, PREFIX><<<grid, kWaves * 64, 0, stream>>>(a);
-    else paged_tile_kernel<D, F16, PREFIX><<<grid, 256, 0, stream>>>(a);
+    Launch a = {};
+    a.p = p;
+    return (size_t)plan(a, head_dim);
 }
 
 template <int D, bool F16> static hipError_t launch(const PagedParams &p, hipStream_t stream)
 {
-    const Plan y = plan_of(p, D);
-    if (p.prefix) attend<D, F16, true>(y.prefix, y.prefix.parts, stream);
-    attend<D, F16, false>(y.own, p.batch + y.own.extra, stream);
-    if (y.own.extra || !y.own.direct)
-        paged_join_kernel<D, F16><<<(unsigned)(p.batch * p.seqlen * p.hq), 256, 0, stream>>>(y.own, p.batch * y.own.rows, y.own.rows);
+    Launch a = {};
+    a.p = p;
+    const bool joined = plan(a, D) > 0;
+    const unsigned own = (unsigned)((int64_t)(a.shares ? a.shares : p.batch * a.parts) * a.groups * p.hkv);
+    const unsigned prefix = (unsigned)((int64_t)a.prefix_parts * a.prefix_groups * p.hkv);
+    const bool tiled_prefix = a.prefix_rows > kFewRows;
+    if (a.rows > kFewRows) {
+        if (prefix) paged_tile_kernel<D, F16, true><<<prefix, 256, 0, stream>>>(a);
+        paged_tile_kernel<D, F16, false><<<own, 256, 0, stream>>>(a);
+    } else if (tiled_prefix) {
+        if (a.rows <= 16) paged_stream_kernel<D, 1, F16, true><<<prefix + own, 256, 0, stream>>>(a);
+        else paged_stream_kernel<D, 2, F16, true><<<prefix + own, 256, 0, stream>>>(a);
+    } else {
+        if (std::max(a.rows, a.prefix_rows) <= 16) paged_stream_kernel<D, 1, F16, false><<<prefix + own, 256, 0, stream>>>(a);
+        else paged_stream_kernel<D, 2, F16, false><<<prefix + own, 256, 0, stream>>>(a);
+    }
+    if (joined) {
+        const int64_t out = (int64_t)p.batch * p.seqlen * p.hq;
+        if (out <= 2048) paged_join_kernel<D, F16, 4><<<(unsigned)out, 256, 0, stream>>>(a);
+        else paged_join_kernel<D, F16, 1><<<(unsigned)((out + 3) / 4), 256, 0, stream>>>(a);
+    }
     return hipGetLastError();
 }
 

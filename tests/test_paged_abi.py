@@ -126,6 +126,15 @@ def test_workspace_follows_the_work(lib):
     assert need(prefix_table=0x10000, prefix_len=20, prefix_pages=2) > 0
 
 
+def test_packed_descriptors_are_the_structures():
+    """The binding packs the descriptors' members by format: at the places that the structures have them."""
+    vals = iter(range(1, 200))
+    for cls, pack in ((binding.bsfa_cache, binding._PACK_CACHE), (binding.bsfa_append, binding._PACK_APPEND), (binding.bsfa_paged, binding._PACK_PAGED)):
+        v = [next(vals) for _ in cls._fields_]
+        packed = pack(*v)
+        assert bytes(cls(*v))[:len(packed)] == packed and ctypes.sizeof(cls) - len(packed) < 8
+
+
 def test_binding_refuses():
     q = torch.zeros(1, 1, 2, 128, dtype=torch.bfloat16)
     kc = torch.zeros(4, 16, 2, 128, dtype=torch.bfloat16)
