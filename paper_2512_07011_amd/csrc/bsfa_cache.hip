@@ -7,32 +7,30 @@
 // or, interleaved, (2i, 2i + 1), i < rot/2.
 //
 // What bounds it: memory (each element is read once and written once; a fused projection's row of 32 + 2 * 8 heads of width
-// 128 is 12 KiB, the table's row 512 bytes).  So a wave takes one token: its lanes are (row, 16 elements), a row being a
+// 128 is 12 KiB, the table's row 512 bytes).  So WPT waves take one token: their lanes are (row, 16 elements), a row being a
 // query, key or value head, and walk the rows with the same 16 elements: the table's values stay in registers for all of
-// the token's heads.  Loads of kRows rows are in flight together, and they do not wait for the position or the page.
+// the token's heads.  kRows rows are in flight together, and they are requested before the position is known, which the
+// table's row and the page wait for.
 #include "bsfa_dev.h"
 
 namespace bsfa {
 
-constexpr int kRows = 3;             // rows a lane has in flight
+constexpr int kRows = 2;             // rows a lane has in flight
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-template <int D, bool F16, bool INTERLEAVED>
+template <int D, bool F16, bool INTERLEAVED, int WPT>
 __global__ void __launch_bounds__(256) append_kernel(const AppendParams p)
 {
     typedef typename Elem<F16>::T el;
     typedef typename Elem<F16>::x8 el8;
     constexpr int TPR = D / 16;                          // lanes of a row
-    constexpr int RPW = 64 / TPR;                        // rows of a wave at a time
-    const int lane = threadIdx.x & 63;
-    const uint32_t tok = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int RPW = 64 * WPT / TPR;                  // rows at a time
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & (64 * WPT - 1);
+    const uint32_t tok = blockIdx.x * (4 / WPT) + wave / WPT;
     if (tok >= (uint32_t)p.batch * (uint32_t)p.seqlen) return;
     const int b = (int)p.div_seqlen.of(tok), i = (int)(tok - (uint32_t)b * (uint32_t)p.seqlen);
     if (p.seqlens && i >= p.seqlens[b]) return;
-    const int64_t pos = (int64_t)p.start[b] + i;
-    if (pos < 0 || pos >= (int64_t)p.table_pages << p.pages.page_log2) return;           // has no place in the table
-    const int page = p.table[b * p.tsb + (pos >> p.pages.page_log2)];
-    const bool stored = page >= 0 && page < p.pages.n_pages;
-    const int64_t place = pos & ((1 << p.pages.page_log2) - 1);
+    const int start = p.start[b];
 
     // this lane's 16 elements of every row: two runs of 8, the halves of 8 pairs (or, interleaved and behind the rotated
     // elements, 16 adjacent ones)
@@ -40,19 +38,9 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendParams p)
     const bool turns = part * 16 < p.rot;
     const int at0 = INTERLEAVED || !turns ? part * 16 : part * 8;
     const int at1 = INTERLEAVED || !turns ? at0 + 8 : at0 + p.rot / 2;
-    float cs[8], sn[8];                                  // of the pairs that begin at at0 (interleaved: half of it)
-    if (turns) {
-        const float *t = p.cos_sin + pos * p.rot + part * 8;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            cs[e] = t[e];
-            sn[e] = t[p.rot / 2 + e];
-        }
-    }
-
     const int hq = p.q ? p.hq : 0, rows = hq + 2 * p.hkv;
-    for (int r0 = lane / TPR; r0 < rows; r0 += RPW * kRows) {
-        el8 lo[kRows], hi[kRows];
+    el8 lo[kRows], hi[kRows];
+    auto load = [&](int r0) {
 #pragma unroll
         for (int n = 0; n < kRows; ++n) {
             const int r = r0 + n * RPW, h = r - hq;
@@ -63,6 +51,24 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendParams p)
             lo[n] = *reinterpret_cast<const el8 *>(src + (value ? part * 16 : at0));
             hi[n] = *reinterpret_cast<const el8 *>(src + (value ? part * 16 + 8 : at1));
         }
+    };
+    load(lane / TPR);
+
+    const int64_t pos = (int64_t)start + i;
+    if (pos < 0 || pos >= (int64_t)p.table_pages << p.pages.page_log2) return;           // has no place in the table
+    const int page = p.table[b * p.tsb + (pos >> p.pages.page_log2)];
+    const bool stored = page >= 0 && page < p.pages.n_pages;
+    const int64_t place = pos & ((1 << p.pages.page_log2) - 1);
+    f32x4 cs[2], sn[2];                                  // of the pairs that begin at at0 (interleaved: half of it)
+    if (turns) {
+        const float *t = p.cos_sin + pos * p.rot + part * 8;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            cs[e] = *reinterpret_cast<const f32x4 *>(t + 4 * e);
+            sn[e] = *reinterpret_cast<const f32x4 *>(t + p.rot / 2 + 4 * e);
+        }
+    }
+    for (int r0 = lane / TPR; r0 < rows;) {
 #pragma unroll
         for (int n = 0; n < kRows; ++n) {
             const int r = r0 + n * RPW, h = r - hq;
@@ -78,17 +84,24 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendParams p)
             if (turns) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
+                    const auto turn = [&](el &x, el &y, int pair) {
+                        const float a = (float)x, c = (float)y, co = cs[pair >> 2][pair & 3], si = sn[pair >> 2][pair & 3];
+                        x = (el)(a * co - c * si);
+                        y = (el)(c * co + a * si);
+                    };
+                    el x, y;
                     if constexpr (INTERLEAVED) {
-                        if (e & 1) continue;
-                        const float a = (float)lo[n][e], c = (float)lo[n][e + 1], a2 = (float)hi[n][e], c2 = (float)hi[n][e + 1];
-                        lo[n][e] = (el)(a * cs[e / 2] - c * sn[e / 2]);
-                        lo[n][e + 1] = (el)(c * cs[e / 2] + a * sn[e / 2]);
-                        hi[n][e] = (el)(a2 * cs[4 + e / 2] - c2 * sn[4 + e / 2]);
-                        hi[n][e + 1] = (el)(c2 * cs[4 + e / 2] + a2 * sn[4 + e / 2]);
+                        x = e < 4 ? lo[n][2 * e] : hi[n][2 * e - 8];
+                        y = e < 4 ? lo[n][2 * e + 1] : hi[n][2 * e - 7];
+                        turn(x, y, e);
+                        if (e < 4) lo[n][2 * e] = x, lo[n][2 * e + 1] = y;
+                        else hi[n][2 * e - 8] = x, hi[n][2 * e - 7] = y;
                     } else {
-                        const float a = (float)lo[n][e], c = (float)hi[n][e];
-                        lo[n][e] = (el)(a * cs[e] - c * sn[e]);
-                        hi[n][e] = (el)(c * cs[e] + a * sn[e]);
+                        x = lo[n][e];
+                        y = hi[n][e];
+                        turn(x, y, e);
+                        lo[n][e] = x;
+                        hi[n][e] = y;
                     }
                 }
             }
@@ -105,22 +118,29 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendParams p)
                     *reinterpret_cast<el8 *>(dst[o] + at1) = hi[n];
                 }
         }
+        r0 += RPW * kRows;
+        if (r0 < rows) load(r0);
     }
 }
 
-template <int D, bool F16> static void launch(const AppendParams &p, unsigned grid, hipStream_t stream)
+template <int D, bool F16, int WPT> static void launch(const AppendParams &p, hipStream_t stream)
 {
-    if (p.interleaved) append_kernel<D, F16, true><<<grid, 256, 0, stream>>>(p);
-    else append_kernel<D, F16, false><<<grid, 256, 0, stream>>>(p);
+    const unsigned grid = (unsigned)(((int64_t)p.batch * p.seqlen * WPT + 3) / 4);
+    if (p.interleaved) append_kernel<D, F16, true, WPT><<<grid, 256, 0, stream>>>(p);
+    else append_kernel<D, F16, false, WPT><<<grid, 256, 0, stream>>>(p);
+}
+template <int D, bool F16> static void launch(const AppendParams &p, hipStream_t stream)
+{
+    if ((int64_t)p.batch * p.seqlen <= 2048) launch<D, F16, 4>(p, stream);
+    else launch<D, F16, 1>(p, stream);
 }
 
 hipError_t launch_append(const AppendParams &params, int head_dim, bool f16, hipStream_t stream)
 {
     AppendParams p = params;
     p.div_seqlen = fast_div((uint32_t)p.seqlen);
-    const unsigned grid = (unsigned)(((int64_t)p.batch * p.seqlen + 3) / 4);
-    if (head_dim == 128) f16 ? launch<128, true>(p, grid, stream) : launch<128, false>(p, grid, stream);
-    else if (head_dim == 64) f16 ? launch<64, true>(p, grid, stream) : launch<64, false>(p, grid, stream);
+    if (head_dim == 128) f16 ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
+    else if (head_dim == 64) f16 ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
     else return hipErrorInvalidValue;
     return hipGetLastError();
 }

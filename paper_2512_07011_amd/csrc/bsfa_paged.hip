@@ -25,18 +25,18 @@ constexpr float kNone = -3.0e38f;    // running maximum of a row that has seen n
 // 32 grows in one tile of five over 32K keys).
 constexpr float kSlack = 8.f;
 constexpr int kSub = 16;             // keys that lie in one page whatever its size
-constexpr int kMinShare = 8;         // sub-blocks of a workgroup, at least
 
 struct Launch {
     PagedParams p;
     // The sequences' own tokens: a unit of `rows` rows each, `groups` workgroups side by side.  shares > 0: the batch's tokens
-    // are dealt to so many workgroups evenly (even_share); 0: every sequence is cut into `parts` ranges.
-    int rows, groups, shares, parts;
+    // are dealt to so many workgroups evenly (even_share), min_share sub-blocks or more each; 0: one to a sequence.
+    int rows, groups, shares, min_share;
     // The prefix: one unit of prefix_rows rows, ranges of prefix_chunk keys.
     int prefix_rows, prefix_groups, prefix_parts, prefix_chunk;
     // Unscaled results of ranges [slot][hkv][rows][d] and their (m, l); slots: see Range, and the prefix's ranges.
     float *own_o, *prefix_o;
     float2 *own_ml, *prefix_ml;
+    int2 *own_ranges;                // shares > 0: first slot and number of ranges of every sequence
     int own_slots;
     bool direct;                     // a sequence in one range is written to out at once
 };
@@ -60,7 +60,7 @@ __device__ __forceinline__ int anew(int x)
 
 // ---- ranges of keys -------------------------------------------------------------------------------------
 struct Range {
-    int b, len;                      // sequence and its tokens
+    int b, len, new_tokens;          // sequence, its tokens, its rows' tokens
     int k0, k1;                      // keys
     int slot;                        // where the result goes ...
     bool whole;                      // ... unless this is all of the sequence
@@ -77,8 +77,22 @@ __device__ __forceinline__ int units_of(int len) { return max(1, (len + kSub - 1
 // grow.
 struct Share {
     int share;                       // sub-blocks of a workgroup
-    int b, before, len;              // a sequence, the sub-blocks before it, its tokens
+    int b, before, len, new_tokens;  // a sequence, the sub-blocks before it, its tokens, its rows' tokens
+    int b0, lens, news;              // of sequence b0 + lane
 };
+__device__ __forceinline__ void load_lengths(Params &p, int b0, int &lens, int &news)
+{
+    const int b = min(b0 + (int)(threadIdx.x & 63), p.batch - 1);
+    lens = length_of(p, b);
+    news = queries_of(p, b);
+}
+__device__ __forceinline__ void take_sequence(Params &p, int b, Share &y)
+{
+    if (b >= y.b0 + 64) load_lengths(p, y.b0 = b, y.lens, y.news);
+    y.b = b;
+    y.len = __builtin_amdgcn_readlane(y.lens, b - y.b0);
+    y.new_tokens = __builtin_amdgcn_readlane(y.news, b - y.b0);
+}
 // sum over lanes 0 .. l: inside rows of 16 lanes, then each row's last lane to the rows behind it
 __device__ __forceinline__ int scan_lanes(int x)
 {
@@ -90,57 +104,90 @@ __device__ __forceinline__ int scan_lanes(int x)
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
     return x;
 }
-// The sequence that holds sub-block x * share, or (BY_SHARE false) sequence x; every wave for itself.  False: there is none.
-template <bool BY_SHARE> __device__ __forceinline__ bool even_share(Args &a, int x, Share &y)
+// The sequence that holds sub-block x * share; every wave for itself.  False: there is none.
+__device__ __forceinline__ bool even_share(Args &a, int x, Share &y)
 {
     Params &p = a.p;
     const int lane = threadIdx.x & 63;
-    auto scan = [&](int b0, int &len, int &upto) {       // sub-blocks of sequences b0 .. b0 + lane
-        len = b0 + lane < p.batch ? length_of(p, b0 + lane) : 0;
-        upto = scan_lanes(b0 + lane < p.batch ? units_of(len) : 0);
-        return __builtin_amdgcn_readlane(upto, 63);
-    };
-    int len, upto, total = scan(0, len, upto);
-    const int first = total;
+    // sub-blocks of sequences b0 .. b0 + lane; all 64 of them
+    auto scan = [&](int b0, int lens) { return scan_lanes(b0 + lane < p.batch ? units_of(lens) : 0); };
+    auto last = [](int upto) { return __builtin_amdgcn_readlane(upto, 63); };
+    y.b0 = 0;
+    load_lengths(p, 0, y.lens, y.news);
+    int upto = scan(0, y.lens), total = last(upto);
     for (int b0 = 64; b0 < p.batch; b0 += 64) {
-        int l, u;
-        total += scan(b0, l, u);
+        int lens, news;
+        load_lengths(p, b0, lens, news);
+        total += last(scan(b0, lens));
     }
-    y.share = (max((total + a.shares - 1) / a.shares, kMinShare) + 3) & ~3;
-    int before = 0, sum = first;
-    for (int b0 = 0; b0 < p.batch; b0 += 64) {
-        if (b0) sum = scan(b0, len, upto);
-        if (BY_SHARE ? (int64_t)x * y.share < before + sum : x < b0 + 64) {
-            const int l = BY_SHARE ? __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > x * y.share)) : x - b0;
-            y.b = b0 + l;
-            y.len = __builtin_amdgcn_readlane(len, l);
+    y.share = max((total + a.shares - 1) / a.shares, a.min_share);
+    int before = 0;
+    while (true) {
+        const int sum = last(upto);
+        if ((int64_t)x * y.share < before + sum) {
+            const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > x * y.share));
+            take_sequence(p, y.b0 + l, y);
             y.before = before + __builtin_amdgcn_readlane(upto, l) - units_of(y.len);
             return true;
         }
         before += sum;
+        if (y.b0 + 64 >= p.batch) return false;
+        load_lengths(p, y.b0 += 64, y.lens, y.news);
+        upto = scan(y.b0, y.lens);
     }
-    return false;
 }
 
-// Range `part` of those that a sequence is cut into.
-__device__ __forceinline__ Range cut_range(Args &a, int x)
+// The sequences' own tokens that are workgroup x's: f for every range.  (KEEP: the lengths that are at hand stay in two
+// vector registers in the meantime, and the next range does not wait for its own.)
+template <bool KEEP, class F> __device__ __forceinline__ void own_ranges(int hk, int x, int rg, F &&f)
 {
-    Range r;
-    r.b = x / a.parts;
-    const int part = x - r.b * a.parts;
-    r.len = __builtin_amdgcn_readfirstlane(length_of(a.p, r.b));
-    const int chunk = ((r.len + a.parts - 1) / a.parts + 63) & ~63;
-    r.k0 = min(part * chunk, r.len);
-    r.k1 = min(r.k0 + chunk, r.len);
-    r.slot = x;
-    r.whole = a.parts == 1;
-    return r;
+    Share y;
+    int from = 0, to = 0x7fffffff;                       // (all of one sequence)
+    {
+        Args &a = arguments();
+        if (a.shares) {
+            if (!even_share(a, x, y)) return;
+            from = x * y.share;
+            to = from + y.share;
+        } else {
+            y.b = x;
+            y.before = y.b0 = 0;
+            y.len = __builtin_amdgcn_readfirstlane(length_of(a.p, x));
+            y.new_tokens = __builtin_amdgcn_readfirstlane(queries_of(a.p, x));
+        }
+    }
+    while (true) {
+        Args &a = arguments();
+        Range r;
+        const int end = y.before + units_of(y.len);
+        r.b = y.b;
+        r.len = y.len;
+        r.new_tokens = y.new_tokens;
+        r.k0 = max(from - y.before, 0) * kSub;
+        r.k1 = end <= to ? r.len : (to - y.before) * kSub;
+        r.slot = a.shares ? x + y.b : x;
+        r.whole = from <= y.before && end <= to;
+        // where the join finds the sequence's ranges
+        if (a.shares && from <= y.before && hk == 0 && rg == 0 && threadIdx.x == 0) a.own_ranges[y.b] = make_int2(r.slot, (end - 1) / y.share - x + 1);
+        f(r);
+        Args &z = arguments();
+        y.before = end;
+        if (!z.shares || end >= to || y.b + 1 >= z.p.batch) return;
+        if constexpr (KEEP) take_sequence(z.p, y.b + 1, y);
+        else {
+            y.len = __builtin_amdgcn_readfirstlane(length_of(z.p, ++y.b));
+            y.new_tokens = __builtin_amdgcn_readfirstlane(queries_of(z.p, y.b));
+        }
+        __syncthreads();                                 // (the LDS is free again)
+    }
 }
+
 __device__ __forceinline__ Range prefix_range(Args &a, int x)
 {
     Range r;
     r.b = 0;
     r.len = a.p.prefix;
+    r.new_tokens = a.p.seqlen;
     r.k0 = x * a.prefix_chunk;
     r.k1 = min(r.k0 + a.prefix_chunk, r.len);
     r.slot = x;
@@ -261,8 +308,8 @@ __device__ __forceinline__ void stream_range(Args &a, const Range r, int hk, int
 
     Params &p = a.p;
     const bool masked = !PREFIX && p.causal;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int qn = PREFIX ? p.seqlen : __builtin_amdgcn_readfirstlane(queries_of(p, r.b));
+    const int lane = anew(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (anew: nothing of a lane's is kept from range to range)
+    const int qn = r.new_tokens;
     const int k0 = r.k0, rows = PREFIX ? a.prefix_rows : a.rows;
     int k1 = r.k1;
     const int row0 = rg * kSub * NRT;
@@ -456,38 +503,6 @@ __device__ __forceinline__ void stream_range(Args &a, const Range r, int hk, int
     }
 }
 
-// The sequences' own tokens: those of workgroup x.
-template <int D, int NRT, bool F16>
-__device__ __forceinline__ void stream_own(Args &a, int hk, int x, int rg, StreamLds<D, NRT> &shared)
-{
-    Range r;
-    Share y;
-    int from = 0, to = 0;
-    if (a.shares) {
-        if (!even_share<true>(a, x, y)) return;
-        from = x * y.share;
-        to = from + y.share;
-    }
-    while (true) {
-        if (a.shares) {
-            const int units = units_of(y.len);
-            r.b = y.b;
-            r.len = y.len;
-            r.k0 = max(from - y.before, 0) * kSub;
-            r.k1 = min(r.len, (to - y.before) * kSub);
-            r.slot = x + y.b;
-            r.whole = from <= y.before && y.before + units <= to;
-            y.before += units;
-        } else {
-            r = cut_range(a, x);
-        }
-        stream_range<D, NRT, F16, false>(a, r, hk, rg, shared);
-        if (!a.shares || y.before >= to || ++y.b >= a.p.batch) return;
-        y.len = __builtin_amdgcn_readfirstlane(length_of(a.p, y.b));
-        __syncthreads();                                 // (the ring is free again)
-    }
-}
-
 // ---- many rows: keys shared by a workgroup's waves ------------------------------------------------------
 // Four waves of 32 rows on tiles of 64 keys, K and V in two LDS slots each; a wave copies the sub-block of its number.
 //   S^T = K Q^T, O^T += V^T P^T with 32x32x16 MFMA, P in registers as above.
@@ -509,14 +524,14 @@ __device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int r
     typedef SubBlock<D> SB;
     constexpr int KS = D / 16, DB = D / 32;              // MFMAs of a score half; 32-row blocks of O^T
     constexpr int NQK = 2 * KS, NPV = 4 * DB, EPM = 32 / NQK;
-    constexpr int PD = 4;                                // operand reads run that many MFMAs ahead
+    constexpr int PD = D == 64 ? 3 : 4;                  // operand reads run that many MFMAs ahead (64: three waves to a SIMD, 168 registers)
     constexpr int SLOT = 4 * SB::BYTES;
     constexpr uint32_t K0 = 0, V0 = 2 * SLOT;
 
     Params &p = a.p;
     const bool causal = !PREFIX && p.causal;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int qn = PREFIX ? p.seqlen : __builtin_amdgcn_readfirstlane(queries_of(p, r.b));
+    const int lane = anew(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (anew: nothing of a lane's is kept from range to range)
+    const int qn = r.new_tokens;
     const int k0 = r.k0, rows = PREFIX ? a.prefix_rows : a.rows;
     int k1 = r.k1;
     const int row0 = rg * kTileRows;
@@ -819,105 +834,96 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_stream_kernel(cons
         if constexpr (TILED_PREFIX) tile_range<D, F16, true>(a, r, w.hk, w.rg, shared.tile);
         else stream_range<D, NRT, F16, true>(a, r, w.hk, w.rg, shared.stream);
     } else {
-        stream_own<D, NRT, F16>(arguments(), w.hk, w.x, w.rg, shared.stream);
+        own_ranges<true>(w.hk, w.x, w.rg, [&](const Range &r) { stream_range<D, NRT, F16, false>(arguments(), r, w.hk, w.rg, shared.stream); });
     }
 }
 
 template <int D, bool F16, bool PREFIX>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) paged_tile_kernel(const Launch)
 {
-    Args &a = arguments();
     __shared__ __attribute__((aligned(1024))) TileLds<D> shared;
+    Args &a = arguments();
     const int hk = blockIdx.x % a.p.hkv, v = blockIdx.x / a.p.hkv, groups = PREFIX ? a.prefix_groups : a.groups;
     const int x = v / groups, rg = groups - 1 - (v - x * groups);          // (later rows see more keys: first)
-    tile_range<D, F16, PREFIX>(a, PREFIX ? prefix_range(a, x) : cut_range(a, x), hk, rg, shared);
+    if constexpr (PREFIX) tile_range<D, F16, true>(a, prefix_range(a, x), hk, rg, shared);
+    else own_ranges<false>(hk, x, rg, [&](const Range &r) { tile_range<D, F16, false>(arguments(), r, hk, rg, shared); });
 }
 
-// Ranges joined: WPR waves to a row of one query head, which take its ranges in turn; a lane has D / 64 elements.
-template <int D, bool F16, int WPR>
+// Ranges joined.  A group of D / 4 lanes (one 16-byte load a lane) takes the ranges of a row of one query head in turn; GPR
+// groups share a row: one where there are many rows, all of the workgroup where there are few, and many ranges.
+template <int D> constexpr int join_groups() { return 256 / (D / 4); }
+template <int D, bool F16, int GPR>
 __global__ void __launch_bounds__(256) paged_join_kernel(const Launch)
 {
     Args &a = arguments();
     typedef typename Elem<F16>::T el;
-    constexpr int E = D / 64, ROWS = 4 / WPR;
-    typedef float fx __attribute__((ext_vector_type(E)));
-    typedef el elx __attribute__((ext_vector_type(E)));
-    __shared__ float red[4][D + 2];
+    typedef el el4 __attribute__((ext_vector_type(4)));
+    constexpr int LANES = D / 4, GROUPS = join_groups<D>();
+    __shared__ f32x4 red_o[GPR > 1 ? GROUPS : 1][LANES];
+    __shared__ float2 red_ml[GROUPS];
     Params &p = a.p;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int id = blockIdx.x * ROWS + (WPR == 4 ? 0 : wave), sub = WPR == 4 ? wave : 0;
+    const int group = threadIdx.x / LANES, at_lane = threadIdx.x % LANES;
+    const int id = GPR > 1 ? blockIdx.x : blockIdx.x * GROUPS + group, sub = GPR > 1 ? group : 0;
     if (id >= p.batch * p.seqlen * p.hq) return;
     const int t = id / p.hq, h = id - t * p.hq, b = t / p.seqlen, i = t - b * p.seqlen;
-    if (i >= __builtin_amdgcn_readfirstlane(queries_of(p, b))) return;
-    int slot = b * a.parts, own = a.parts;               // the sequence's ranges
-    if (a.shares) {
-        Share y;
-        even_share<false>(a, b, y);
-        const int w0 = y.before / y.share;
-        own = (y.before + units_of(y.len) - 1) / y.share - w0 + 1;
-        slot = w0 + b;
-    }
-    if (a.direct && own == 1) return;                    // written already
+    const int2 mine = a.shares ? a.own_ranges[b] : make_int2(b, 1);      // the sequence's ranges
+    const int own = mine.y;
+    if (i >= queries_of(p, b) || (a.direct && own == 1)) return;         // (written already)
     const int hk = h / p.group, g = h - hk * p.group;
-    const int64_t own_at = ((int64_t)slot * p.hkv + hk) * a.rows + i * p.group + g;
+    const int64_t own_at = ((int64_t)mine.x * p.hkv + hk) * a.rows + i * p.group + g;
     const int64_t prefix_at = (int64_t)hk * a.prefix_rows + ((int64_t)b * p.seqlen + i) * p.group + g;
     const int64_t own_step = (int64_t)p.hkv * a.rows, prefix_step = (int64_t)p.hkv * a.prefix_rows;
     const int n = a.prefix_parts + own;
     float m = kNone, l = 0.f;
-    fx o;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
     constexpr int AT_ONCE = 4;
-    for (int y0 = sub; y0 < n; y0 += AT_ONCE * WPR) {
+    for (int y0 = sub; y0 < n; y0 += AT_ONCE * GPR) {
         float2 ml[AT_ONCE];
-        fx v[AT_ONCE];
+        f32x4 v[AT_ONCE];
 #pragma unroll
         for (int c = 0; c < AT_ONCE; ++c) {
-            const int y = min(y0 + c * WPR, n - 1);
+            const int y = min(y0 + c * GPR, n - 1);
             const bool pre = y < a.prefix_parts;
             const int64_t at = pre ? prefix_at + y * prefix_step : own_at + (y - a.prefix_parts) * own_step;
             ml[c] = (pre ? a.prefix_ml : a.own_ml)[at];
-            if (y0 + c * WPR >= n) ml[c] = make_float2(kNone, 0.f);
-            v[c] = *reinterpret_cast<const fx *>((pre ? a.prefix_o : a.own_o) + at * D + lane * E);
+            if (y0 + c * GPR >= n) ml[c] = make_float2(kNone, 0.f);      // (a repeated last range counts for nothing)
+            v[c] = *reinterpret_cast<const f32x4 *>((pre ? a.prefix_o : a.own_o) + at * D + at_lane * 4);
         }
         float mm = m;
 #pragma unroll
         for (int c = 0; c < AT_ONCE; ++c) mm = fmaxf(mm, ml[c].x);
         const float f = __builtin_amdgcn_exp2f(m - mm);
         l *= f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= f;
+        o *= f;
 #pragma unroll
         for (int c = 0; c < AT_ONCE; ++c) {
-            // (a repeated last range counts for nothing)
-            const float w = y0 + c * WPR < n ? __builtin_amdgcn_exp2f(ml[c].x - mm) : 0.f;
+            const float w = y0 + c * GPR < n ? __builtin_amdgcn_exp2f(ml[c].x - mm) : 0.f;
             l = fmaf(ml[c].y, w, l);
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = fmaf(v[c][e], w, o[e]);
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(v[c][e], w, o[e]);
         }
         m = mm;
     }
-    if constexpr (WPR == 4) {
-        red[wave][D] = m;
-        red[wave][D + 1] = l;
-#pragma unroll
-        for (int e = 0; e < E; ++e) red[wave][lane * E + e] = o[e];
+    if constexpr (GPR > 1) {
+        red_o[group][at_lane] = o;
+        if (at_lane == 0) red_ml[group] = make_float2(m, l);
         __syncthreads();
-        if (wave != 0) return;
-        for (int y = 1; y < 4; ++y) {
-            const float my = red[y][D], mm = fmaxf(m, my), f = __builtin_amdgcn_exp2f(m - mm), f2 = __builtin_amdgcn_exp2f(my - mm);
-            l = l * f + red[y][D + 1] * f2;
+        if (group != 0) return;
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = o[e] * f + red[y][lane * E + e] * f2;
-            m = mm;
+        for (int y = 0; y < GROUPS; ++y) m = fmaxf(m, red_ml[y].x);
+        l = 0.f;
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int y = 0; y < GROUPS; ++y) {
+            const float w = __builtin_amdgcn_exp2f(red_ml[y].x - m);
+            l = fmaf(red_ml[y].y, w, l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(red_o[y][at_lane][e], w, o[e]);
         }
     }
     const float f = l > 0.f ? 1.f / l : 0.f;
-    elx z;
-#pragma unroll
-    for (int e = 0; e < E; ++e) z[e] = (el)(o[e] * f);
-    *reinterpret_cast<elx *>(p.out + b * p.osb + i * p.osn + h * p.osh + lane * E) = z;
-    if (p.lse && lane == 0) p.lse[((int64_t)b * p.seqlen + i) * p.hq + h] = natural_lse(m, l);
+    *reinterpret_cast<el4 *>(p.out + b * p.osb + i * p.osn + h * p.osh + at_lane * 4) = el4{(el)(o[0] * f), (el)(o[1] * f), (el)(o[2] * f), (el)(o[3] * f)};
+    if (p.lse && at_lane == 0) p.lse[((int64_t)b * p.seqlen + i) * p.hq + h] = natural_lse(m, l);
 }
 
 // ---- launch -----------------------------------------------------------------------------------------------
@@ -934,16 +940,10 @@ static int64_t plan(Launch &a, int head_dim)
     a.groups = row_groups(a.rows);
     a.direct = p.prefix == 0;
     const int64_t side = (int64_t)p.hkv * a.groups, items = p.batch * side;
-    a.parts = 1;
-    a.shares = 0;
-    if (p.max_len > 256) {
-        if (a.rows <= kFewRows) {
-            if (items < 4 * kCus) a.shares = (int)std::max<int64_t>(1, kCus / side);
-        } else {
-            a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(2 * kCus / items, p.max_len / 256));
-        }
-    }
-    a.own_slots = a.shares ? a.shares + p.batch : p.batch * a.parts;
+    const bool few = a.rows <= kFewRows;
+    a.min_share = few ? 4 : 16;
+    a.shares = p.max_len > 256 && items < (few ? 4 : 2) * kCus ? (int)std::max<int64_t>(1, (few ? 1 : 2) * kCus / side) : 0;
+    a.own_slots = a.shares + p.batch;
     if (p.prefix) {
         a.prefix_rows = p.batch * a.rows;
         a.prefix_groups = row_groups(a.prefix_rows);
@@ -952,14 +952,15 @@ static int64_t plan(Launch &a, int head_dim)
         a.prefix_chunk = std::max(128, (int)((p.prefix + want - 1) / want + 63) / 64 * 64);
         a.prefix_parts = (p.prefix + a.prefix_chunk - 1) / a.prefix_chunk;
     }
-    const bool joined = a.shares || a.parts > 1 || p.prefix;
+    const bool joined = a.shares || p.prefix;
     const int64_t own = joined ? (int64_t)a.own_slots * p.hkv * a.rows : 0, prefix = (int64_t)a.prefix_parts * p.hkv * a.prefix_rows;
     unsigned char *at = p.workspace;
     a.own_o = reinterpret_cast<float *>(at);
     a.own_ml = reinterpret_cast<float2 *>(at += up256(own * head_dim * 4));
     a.prefix_o = reinterpret_cast<float *>(at += up256(own * 8));
     a.prefix_ml = reinterpret_cast<float2 *>(at += up256(prefix * head_dim * 4));
-    return at + up256(prefix * 8) - p.workspace;
+    a.own_ranges = reinterpret_cast<int2 *>(at += up256(prefix * 8));
+    return at + (a.shares ? up256((int64_t)p.batch * 8) : 0) - p.workspace;
 }
 
 size_t paged_workspace_bytes(const PagedParams &p, int head_dim)
@@ -974,7 +975,7 @@ template <int D, bool F16> static hipError_t launch(const PagedParams &p, hipStr
     Launch a = {};
     a.p = p;
     const bool joined = plan(a, D) > 0;
-    const unsigned own = (unsigned)((int64_t)(a.shares ? a.shares : p.batch * a.parts) * a.groups * p.hkv);
+    const unsigned own = (unsigned)((int64_t)(a.shares ? a.shares : p.batch) * a.groups * p.hkv);
     const unsigned prefix = (unsigned)((int64_t)a.prefix_parts * a.prefix_groups * p.hkv);
     const bool tiled_prefix = a.prefix_rows > kFewRows;
     if (a.rows > kFewRows) {
@@ -989,8 +990,9 @@ template <int D, bool F16> static hipError_t launch(const PagedParams &p, hipStr
     }
     if (joined) {
         const int64_t out = (int64_t)p.batch * p.seqlen * p.hq;
-        if (out <= 2048) paged_join_kernel<D, F16, 4><<<(unsigned)out, 256, 0, stream>>>(a);
-        else paged_join_kernel<D, F16, 1><<<(unsigned)((out + 3) / 4), 256, 0, stream>>>(a);
+        constexpr int GROUPS = join_groups<D>();
+        if (out <= 2048) paged_join_kernel<D, F16, GROUPS><<<(unsigned)out, 256, 0, stream>>>(a);
+        else paged_join_kernel<D, F16, 1><<<(unsigned)((out + GROUPS - 1) / GROUPS), 256, 0, stream>>>(a);
     }
     return hipGetLastError();
 }
