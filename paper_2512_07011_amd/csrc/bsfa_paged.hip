@@ -30,7 +30,7 @@ struct Launch {
     PagedParams p;
     // The sequences' own tokens: a unit of `rows` rows each, `groups` workgroups side by side.  shares > 0: the batch's tokens
     // are dealt to so many workgroups evenly (even_share), min_share sub-blocks or more each; 0: one to a sequence.
-    int rows, groups, shares, min_share;
+    int rows, groups, shares, min_share, near;
     // The prefix: one unit of prefix_rows rows, ranges of prefix_chunk keys.
     int prefix_rows, prefix_groups, prefix_parts, prefix_chunk;
     // Unscaled results of ranges [slot][hkv][rows][d] and their (m, l); slots: see Range, and the prefix's ranges.
@@ -72,11 +72,12 @@ __device__ __forceinline__ int queries_of(Params &p, int b) { return p.q_lens ? 
 __device__ __forceinline__ int units_of(int len) { return max(1, (len + kSub - 1) / kSub); }
 
 // The batch's sub-blocks in a row, dealt to `shares` workgroups evenly: workgroup x has those from x * share on, which may
-// begin and end inside sequences.  A workgroup or a sequence begins with every range, so the range of workgroup x in
-// sequence b has slot x + b.  The shares follow from the lengths on the device: a captured launch stays even as sequences
-// grow.
+// begin and end inside sequences.  A border between two workgroups that lies no more than `near` sub-blocks from a border
+// between two sequences is moved there: a range more costs more than that.  A workgroup or a sequence begins with every
+// range, so the range of workgroup x in sequence b has slot x + b.  The shares follow from the lengths on the device: a
+// captured launch stays even as sequences grow.
 struct Share {
-    int share;                       // sub-blocks of a workgroup
+    int share, near;                 // sub-blocks of a workgroup; see above
     int b, before, len, new_tokens;  // a sequence, the sub-blocks before it, its tokens, its rows' tokens
     int b0, lens, news;              // of sequence b0 + lane
 };
@@ -121,6 +122,7 @@ __device__ __forceinline__ bool even_share(Args &a, int x, Share &y)
         total += last(scan(b0, lens));
     }
     y.share = max((total + a.shares - 1) / a.shares, a.min_share);
+    y.near = min(a.near, y.share / 4);
     int before = 0;
     while (true) {
         const int sum = last(upto);
@@ -160,16 +162,27 @@ template <bool KEEP, class F> __device__ __forceinline__ void own_ranges(int hk,
         Args &a = arguments();
         Range r;
         const int end = y.before + units_of(y.len);
+        // borders moved to this sequence's: where it begins or ends close to them
+        int lo = from, hi = to;
+        if (a.shares) {
+            if (lo > y.before) lo = lo - y.before <= y.near ? y.before : end - lo <= y.near ? end : lo;
+            if (hi < end) hi = hi - y.before <= y.near ? y.before : end - hi <= y.near ? end : hi;
+        }
+        if (hi <= y.before) return;                      // (the next workgroup's)
         r.b = y.b;
         r.len = y.len;
         r.new_tokens = y.new_tokens;
-        r.k0 = max(from - y.before, 0) * kSub;
-        r.k1 = end <= to ? r.len : (to - y.before) * kSub;
+        r.k0 = max(lo - y.before, 0) * kSub;
+        r.k1 = end <= hi ? r.len : (hi - y.before) * kSub;
         r.slot = a.shares ? x + y.b : x;
-        r.whole = from <= y.before && end <= to;
-        // where the join finds the sequence's ranges
-        if (a.shares && from <= y.before && hk == 0 && rg == 0 && threadIdx.x == 0) a.own_ranges[y.b] = make_int2(r.slot, (end - 1) / y.share - x + 1);
-        f(r);
+        r.whole = lo <= y.before && end <= hi;
+        // where the join finds the sequence's ranges: the borders behind this one that lie inside it begin one each
+        if (a.shares && lo <= y.before && hk == 0 && rg == 0 && threadIdx.x == 0)
+            a.own_ranges[y.b] = make_int2(r.slot, max((end - y.near - 1) / y.share - x, 0) + 1);
+        if (lo < end) {                                  // (else the workgroup before has all of it)
+            f(r);
+            __syncthreads();                             // (the LDS is free again)
+        }
         Args &z = arguments();
         y.before = end;
         if (!z.shares || end >= to || y.b + 1 >= z.p.batch) return;
@@ -178,7 +191,6 @@ template <bool KEEP, class F> __device__ __forceinline__ void own_ranges(int hk,
             y.len = __builtin_amdgcn_readfirstlane(length_of(z.p, ++y.b));
             y.new_tokens = __builtin_amdgcn_readfirstlane(queries_of(z.p, y.b));
         }
-        __syncthreads();                                 // (the LDS is free again)
     }
 }
 
@@ -761,6 +773,7 @@ __device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int r
     }
 
     // ---- results, through the LDS so that rows are written in whole lines ---------------------------------------
+    wait_vmcnt<0>();                                     // (the copies of tiles of nothing write their zeros, too)
     wg_barrier();
     l += __shfl_xor(l, 32);
     Args &z = arguments();
@@ -942,6 +955,7 @@ static int64_t plan(Launch &a, int head_dim)
     const int64_t side = (int64_t)p.hkv * a.groups, items = p.batch * side;
     const bool few = a.rows <= kFewRows;
     a.min_share = few ? 4 : 16;
+    a.near = 8;
     a.shares = p.max_len > 256 && items < (few ? 4 : 2) * kCus ? (int)std::max<int64_t>(1, (few ? 1 : 2) * kCus / side) : 0;
     a.own_slots = a.shares + p.batch;
     if (p.prefix) {

@@ -82,6 +82,33 @@ def test_ranges_joined(lens):
     run_case(lens, 2, 4, 4, 64, 16, "fp16", q_lens=[2 - b % 3 % 2 for b in range(len(lens))])
 
 
+@pytest.mark.parametrize("tiles", [1, 2, 3, 4, 5, 6, 8])
+@pytest.mark.parametrize("d", [64, 128])
+def test_even_and_odd_numbers_of_tiles(tiles, d):
+    """The kernel of many rows looks a tile ahead, at the end at one that does not exist, whose zeros must not come late.  Many
+    workgroups at a time, and results that are dense enough to show a lost row anywhere."""
+    for page in (16, 128):
+        run_case([64 * tiles - 3] * 40, 9, 32, 8, d, page, "bf16", "hnd", max_cache_len=64 * tiles)
+        run_case([5] * 95, 1, 32, 8, d, page, "bf16", prefix=64 * tiles - 16, max_cache_len=16)
+    run_case([64 * tiles + 589] * 2, 589, 4, 2, d, 128, "fp16", "hnd")
+
+
+def _dealt(name):
+    g = torch.Generator().manual_seed(len(name))
+    rnd = lambda n, hi: torch.randint(0, hi, (n,), generator=g).tolist()
+    return {"equal": [340] * 5, "one long": rnd(20, 40) + [4000] + rnd(20, 40), "many": rnd(130, 200) + [0] * 3, "odd": [1, 2500, 0, 17, 16, 900, 15, 901],
+            "borders": [256, 257, 255, 512, 496, 528, 1024, 1, 1023], "empty": [0] * 70, "last": [0] * 64 + [700]}[name]
+
+
+@pytest.mark.parametrize("name", ["equal", "one long", "many", "odd", "borders", "empty", "last"])
+@pytest.mark.parametrize("s,hq,hkv,d", [(1, 1, 1, 128), (1, 8, 8, 64), (3, 8, 1, 128), (5, 16, 2, 64), (9, 16, 2, 128)])
+def test_a_batch_dealt_to_the_chip(name, s, hq, hkv, d):
+    """Sequences of different lengths share workgroups, and workgroups share sequences: 3 x 8 and 5 x 8 and 9 x 8 rows to a KV head
+    take the streaming kernel's wide form and the kernel of many rows."""
+    lens = _dealt(name)
+    run_case(lens, s, hq, hkv, d, 16, "bf16" if d == 128 else "fp16", columns=max(17, -(-max(lens) // 16)))
+
+
 def test_many_sequences_one_range_each():
     lens = [(7 * i) % 300 for i in range(600)]
     run_case(lens, 1, 4, 2, 64, 16)
