@@ -393,14 +393,15 @@ def _same_device(name, q, *ts):
             raise ValueError("%s: tensors must live on one GPU" % name)
 
 
-def _on_device(device, call, *args):
-    """call(*args) with `device` current: the kernels of a stream are launched from its own device."""
-    if device.index == torch.cuda.current_device():
-        rc = call(*args)
+def _on_device(device, stream, call, *args):
+    """call(*args, stream) with `device` current: the kernels of a stream are launched from its own device."""
+    index = device.index
+    if index == torch.cuda.current_device():
+        rc = call(*args, _raw_stream(stream, device))
     else:
         with torch.cuda.device(device):
-            rc = call(*args)
-    if rc != BSFA_OK:
+            rc = call(*args, _raw_stream(stream, device))
+    if rc:
         _check(rc)
 
 
@@ -423,10 +424,10 @@ def _strides(name, t, shape):
     """Strides of a [B, N, H, d] tensor (batch, token, head)."""
     if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, list(t.shape), list(shape)))
-    b, n, h, one = t.stride()
-    if one != 1:
+    stride = t.stride()
+    if stride[3] != 1:
         raise ValueError("%s: head dimension must be contiguous" % name)
-    return b, n, h
+    return stride[:3]
 
 
 def _cache(name, k_cache, v_cache):
@@ -489,7 +490,7 @@ def bsfa_cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
                      0 if seqlens is None else _lens("seqlens", seqlens, B), _lens("start", start, B), table, table_stride, pages,
                      cs_ptr, positions, rot, 1 if interleaved else 0)
     device = k.device
-    _on_device(device, lib().bsfa_cache_append, c, p, q_ptr, k.data_ptr(), v.data_ptr(), qo_ptr, ko_ptr, _raw_stream(stream, device))
+    _on_device(device, stream, lib().bsfa_cache_append, c, p, q_ptr, k.data_ptr(), v.data_ptr(), qo_ptr, ko_ptr)
     return q_out, k_out
 
 
@@ -536,8 +537,7 @@ def _attend(call, name, q, k_cache, v_cache, prefix_table, prefix_len, block_tab
         _same_device(name, q, workspace)
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     device = q.device
-    _on_device(device, call, c, _PACK_PAGED(*members, ws_ptr, ws_bytes), q.data_ptr(), 1 if causal else 0, out.data_ptr(), lse_ptr,
-               _raw_stream(stream, device))
+    _on_device(device, stream, call, c, _PACK_PAGED(*members, ws_ptr, ws_bytes), q.data_ptr(), 1 if causal else 0, out.data_ptr(), lse_ptr)
     return out
 
 

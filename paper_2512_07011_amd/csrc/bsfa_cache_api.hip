@@ -14,6 +14,7 @@ using bsfa::fail_with;
 bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 constexpr int64_t kMaxPlaces = 1 << 30;                 // of one block table
+constexpr int64_t kMaxTokens = 1 << 25, kMaxRows = 1 << 26, kMaxUnits = 1 << 23;      // (grids of less than 2^32 threads)
 constexpr int64_t kMaxTokenStride = 1 << 25;            // a copy addresses 16 tokens of a page with 32-bit offsets
 
 // strides of a tensor's dimensions that have more than one element (those of the others are never used)
@@ -57,7 +58,9 @@ bsfa_status check_batch(const bsfa_cache *c, int batch, int hq, int seqlen)
 {
     if (batch < 1 || hq < 1 || seqlen < 1) FAIL(BSFA_ERR_SHAPE, "batch, n_q_heads and seqlen must be positive");
     if (hq % c->n_kv_heads) FAIL(BSFA_ERR_SHAPE, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", hq, c->n_kv_heads);
-    if ((int64_t)batch * seqlen > kMaxPlaces / hq) FAIL(BSFA_ERR_SHAPE, "batch * seqlen * n_q_heads exceeds 2^30 rows");
+    if ((int64_t)batch * seqlen > kMaxTokens) FAIL(BSFA_ERR_SHAPE, "batch * seqlen exceeds 2^25 tokens");
+    if ((int64_t)batch * seqlen * hq > kMaxRows) FAIL(BSFA_ERR_SHAPE, "batch * seqlen * n_q_heads exceeds 2^26 rows");
+    if ((int64_t)batch * c->n_kv_heads > kMaxUnits) FAIL(BSFA_ERR_SHAPE, "batch * n_kv_heads exceeds 2^23");
     return BSFA_OK;
 }
 
@@ -83,6 +86,7 @@ bsfa_status check_paged(const bsfa_cache *c, const bsfa_paged *p, bool prefix)
     if (s != BSFA_OK) return s;
     if (prefix && (p->prefix_len < 1 || p->prefix_len > (int64_t)p->prefix_pages * c->page_size))
         FAIL(BSFA_ERR_SHAPE, "prefix_len %d must be positive and fit %d pages of %d tokens", p->prefix_len, p->prefix_pages, c->page_size);
+    if ((int64_t)p->batch * p->table_pages * (c->page_size / 16) > kMaxPlaces) FAIL(BSFA_ERR_SHAPE, "the block tables of the batch hold more than 2^34 places");
     if (p->max_cache_len < 0) FAIL(BSFA_ERR_SHAPE, "max_cache_len must not be negative");
     if (misaligned(p->q_lens, 4) || misaligned(p->cache_lens, 4)) FAIL(BSFA_ERR_SHAPE, "q_lens and cache_lens must be 4-byte aligned");
     if (p->workspace_bytes < 0) FAIL(BSFA_ERR_WORKSPACE, "workspace_bytes must not be negative");

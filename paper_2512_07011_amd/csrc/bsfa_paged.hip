@@ -6,6 +6,13 @@
 //     m = max m_x,  l = sum l_x 2^(m_x - m),  O = sum O_x 2^(m_x - m)          (log2 units).
 // The (query token, query head) pairs that read one KV head are the rows of a unit: one sequence's, or for the prefix
 // everybody's.
+//
+// What bounds it.  Few rows to a key (decoding: the query heads of a KV head, 512 bytes of K and V for 4 d times as many
+// operations): memory.  64 sequences of 1K to 8K tokens, 905 MB: 163 us, 5.6 TB/s; two of 128K, 1.07 GB: 185 us, 5.8 TB/s (a
+// large copy moves 4.9 TB/s on the same card, read and written bytes together).  Many rows (a chunk of a prompt, a batch behind one
+// prefix): the matrix pipe and the exponentials beside it.  2048 tokens behind 30K of 32 heads: 965 to 1000 us, 1.07 to 1.11
+// PFLOP/s, the pipe busy in 53 % of the cycles at 1.8 GHz (a large library product reaches 1.32 PFLOP/s).  Small calls: their chain of dependent trips to memory --
+// lengths, page, keys, the ranges' results -- 9 us for a thousand tokens.
 #include "bsfa_dev.h"
 
 #include <algorithm>
@@ -286,12 +293,13 @@ template <bool PREFIX> __device__ __forceinline__ Row row_of(int rows, int group
 __device__ __forceinline__ float natural_lse(float m, float l) { return l > 0.f ? 0.6931471805599453f * (m + __builtin_amdgcn_logf(l)) : -INFINITY; }
 
 // ---- few rows: keys streamed once ---------------------------------------------------------------------
-// A workgroup is NW waves on 16 * NRT rows of one unit and one range of keys.  Every wave takes tiles of 32 keys of its own
-// (the wave-th of every NW), with a ring of kStages tiles in LDS that only it reads: no barrier until the waves' results
-// are joined at the end.
-//   S^T = K Q^T   16x16x32 MFMA, fp32; column = row of the unit, so that a row's scores lie in four lanes
-//   O^T += V^T P^T, V^T through the transposing LDS read; the accumulator layout of S^T is the operand layout of P^T up to
-//   an order of the keys that V's reads share, so P never leaves the registers.
+// A workgroup is four waves on 16 * NRT rows of one unit and one range of keys.  Every wave takes tiles of 16 keys of its own
+// (every fourth), with a ring of kStages tiles in LDS that only it reads: no barrier until the waves' results are joined at
+// the end, and K and V go from memory to LDS without a register.  16 keys and two workgroups to a CU, or 32 keys and one, have
+// the same bytes in flight, but two hide each other's beginnings and ends (256 sequences of 40 to 400 tokens 49 / 31 us, 128K tokens alike).
+//   S^T = K Q^T     16x16x32 MFMA, fp32; column = row of the unit, so that a row's scores lie in four lanes
+//   O^T += V^T P^T  16x16x16 MFMA, V^T through the transposing LDS read; the accumulator layout of S^T is the operand layout
+//                   of P^T, so P never leaves the registers
 // Rounded: P to the element type for the second product (its operands have it); l sums the unrounded fp32 values.
 constexpr int kStages = 2;
 constexpr int kWaves = 4;
@@ -642,6 +650,10 @@ __device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int r
     };
     auto prob = [&](const Scores &z, int n) { return __builtin_amdgcn_exp2f(fmaf(z.s[n >> 4][n & 15], p.scale_log2, -m)); };
 
+    // Of a SIMD's waves the one between the exponentials goes first: it is the way to the next barrier, and the matrix pipe has
+    // work queued by the other (not / so, us: 2048 tokens behind 30K 1034 / 998, 4096 from nothing 158 / 149, 2048 of width 64 348 / 326; not for a
+    // prefix, whose workgroups run beside streaming ones: 4 tokens each of 64 sequences behind 32K 155 / 158, 256 behind 16K 181 / 180).
+    constexpr bool PRIO = !PREFIX;
     el8 kpre[PD];
     int t1, t2, t3;                                      // pages of tiles j + 1, j + 2, j + 3
     // Stage j on the slots of its parity: cur -> P, next <- scores of tile j + 1, if there is one.
@@ -685,6 +697,7 @@ __device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int r
         if constexpr (!LAST) masked(next, j + 1, t1);
         wait_vmcnt<0>();
         wg_barrier();
+        if constexpr (PRIO) __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         el8 vo[NPV + PD];
 #pragma unroll
@@ -729,6 +742,7 @@ __device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int r
             }
             __builtin_amdgcn_sched_barrier(0);
         });
+        if constexpr (PRIO && !LAST) __builtin_amdgcn_s_setprio(1);
     };
 
     if (n_tiles > 0) {
@@ -771,6 +785,8 @@ __device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int r
         }
         if (n_tiles & 1) stage(std::integral_constant<int, 0>{}, std::true_type{}, even, odd, n_tiles - 1);
     }
+
+    if constexpr (PRIO) __builtin_amdgcn_s_setprio(0);
 
     // ---- results, through the LDS so that rows are written in whole lines ---------------------------------------
     wait_vmcnt<0>();                                     // (the copies of tiles of nothing write their zeros, too)
@@ -941,7 +957,10 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const Launch)
 
 // ---- launch -----------------------------------------------------------------------------------------------
 constexpr int kCus = 256;
-constexpr int kFewRows = 32;         // up to that many rows of a unit are streamed
+// Up to that many rows of a unit are streamed; three or four 16-row sets of accumulators do not fit the registers of two waves to a
+// SIMD (streamed / with the kernel of many rows, us, 32 rows: 8 sequences of 2K to 8K tokens 37 / 42, two of 32K 51 / 54, 24 of 700 to 6000
+// of width 64 25.5 / 32.4, but 64 of 100 to 500 30 / 25; 16 rows: 16 of 1K to 4K 31 / 39).
+constexpr int kFewRows = 32;
 static int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 static int row_groups(int rows) { return rows <= kFewRows ? 1 : (rows + kTileRows - 1) / kTileRows; }
 
@@ -954,6 +973,10 @@ static int64_t plan(Launch &a, int head_dim)
     a.direct = p.prefix == 0;
     const int64_t side = (int64_t)p.hkv * a.groups, items = p.batch * side;
     const bool few = a.rows <= kFewRows;
+    // Dealt evenly, one workgroup of the streaming kernel to a CU, two of the other; one workgroup to a sequence where sequences
+    // fill the chip four times over (twice) anyway, whose results need no joining (dealt / not, us: 64 sequences of 1K to 8K tokens, 512
+    // places, 162 / 183, of 2K each 98 / 95; 96 of 300 to 6000, 768, 140 / 155; 128 of 300 to 1500, 1024, 82 / 79; two workgroups of the
+    // streaming kernel to a CU: 64 of 1K to 8K 166, two of 128K 188 instead of 185).
     a.min_share = few ? 4 : 16;
     a.near = 8;
     a.shares = p.max_len > 256 && items < (few ? 4 : 2) * kCus ? (int)std::max<int64_t>(1, (few ? 1 : 2) * kCus / side) : 0;
@@ -962,7 +985,11 @@ static int64_t plan(Launch &a, int head_dim)
         a.prefix_rows = p.batch * a.rows;
         a.prefix_groups = row_groups(a.prefix_rows);
         const int64_t units = (int64_t)p.hkv * a.prefix_groups;
-        const int64_t want = std::max<int64_t>(1, (units <= kCus / 4 ? 1 : 2) * kCus / units);
+        // One workgroup of the prefix to a CU leaves the other place to the own tokens, which then arrive while the prefix is
+        // multiplied; two multiply faster, which counts where that takes longest (one / two, us: 64 sequences behind 32K 64 / 75,
+        // 256 behind 16K 99 / 113, 128 behind 32K 93 / 90; 4 tokens each of 64 behind 32K 165 / 144, two of 256 behind 16K 180 / 173).
+        const bool long_products = units * p.prefix > (int64_t)96 * kTileKeys * kCus;
+        const int64_t want = std::max<int64_t>(1, (long_products ? 2 : 1) * kCus / units);
         a.prefix_chunk = std::max(128, (int)((p.prefix + want - 1) / want + 63) / 64 * 64);
         a.prefix_parts = (p.prefix + a.prefix_chunk - 1) / a.prefix_chunk;
     }

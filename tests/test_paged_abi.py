@@ -89,6 +89,7 @@ def test_append_pointers(lib):
 
 @pytest.mark.parametrize("kw, code", [
     (dict(batch=0), -2), (dict(seqlen=0), -2), (dict(n_q_heads=5), -2), (dict(batch=1 << 20, seqlen=1 << 20), -2), (dict(q_stride_b=-8), -2),
+    (dict(batch=1 << 25, seqlen=1), -2), (dict(seqlen=1 << 25), -2), (dict(batch=1 << 20, seqlen=1, table_pages=1 << 11), -2),
     (dict(q_stride_h=4), -2), (dict(o_stride_n=120), -2), (dict(q_lens=0x10002), -2), (dict(cache_lens=None), -1), (dict(cache_lens=0x10003), -2),
     (dict(block_table=None), -1), (dict(table_pages=0), -2), (dict(table_pages=1 << 27), -2), (dict(table_stride_b=-8), -2), (dict(max_cache_len=-1), -2),
     (dict(workspace_bytes=-1), -5),
