@@ -393,10 +393,12 @@ def _same_device(name, q, *ts):
             raise ValueError("%s: tensors must live on one GPU" % name)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device     # (0.1 us less; no public name)
+
+
 def _on_device(device, stream, call, *args):
     """call(*args, stream) with `device` current: the kernels of a stream are launched from its own device."""
-    index = device.index
-    if index == torch.cuda.current_device():
+    if device.index == _current_device():
         rc = call(*args, _raw_stream(stream, device))
     else:
         with torch.cuda.device(device):
@@ -435,8 +437,10 @@ def _cache(name, k_cache, v_cache):
     shape, dtype = k_cache.shape, k_cache.dtype
     if len(shape) != 4 or dtype not in DTYPES or v_cache.dtype is not dtype:
         raise TypeError("%s: k_cache and v_cache must be [n_pages, page_size, n_kv_heads, head_dim], both bfloat16 or both float16" % name)
-    return _PACK_CACHE(*shape, DTYPES[dtype], *_strides("k_cache", k_cache, shape), *_strides("v_cache", v_cache, shape),
-                       k_cache.data_ptr(), v_cache.data_ptr()), shape, dtype
+    ks, vs = k_cache.stride(), v_cache.stride()
+    if v_cache.shape != shape or ks[3] != 1 or vs[3] != 1:
+        _strides("k_cache", k_cache, shape), _strides("v_cache", v_cache, shape)         # (raises)
+    return _PACK_CACHE(*shape, DTYPES[dtype], *ks[:3], *vs[:3], k_cache.data_ptr(), v_cache.data_ptr()), shape, dtype
 
 
 def bsfa_cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -461,6 +465,9 @@ def bsfa_cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
         raise ValueError("%s: k has shape %s, expected [B, N, %d, %d]" % (name, list(shape), Hkv, d))
     if k.dtype is not dtype or v.dtype is not dtype or (k_out is not None and k_out.dtype is not dtype):
         raise TypeError("%s: tensors and cache must be of one type" % name)
+    ks, vs = k.stride(), v.stride()
+    if v.shape != shape or ks[3] != 1 or vs[3] != 1:
+        _strides("k", k, shape), _strides("v", v, shape)                                 # (raises)
     B, N, Hq = shape[0], shape[1], Hkv
     qs = qos = kos = (0, 0, 0)
     q_ptr = qo_ptr = ko_ptr = cs_ptr = positions = rot = 0
@@ -475,7 +482,9 @@ def bsfa_cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
         if q.dtype is not dtype or q_out.dtype is not dtype:
             raise TypeError("%s: tensors and cache must be of one type" % name)
         Hq = q_shape[2]
-        qs, qos = _strides("q", q, q_shape), _strides("q_out", q_out, q_shape)
+        qs, qos = q.stride(), q_out.stride()
+        if q_out.shape != q_shape or qs[3] != 1 or qos[3] != 1:
+            _strides("q", q, q_shape), _strides("q_out", q_out, q_shape)                 # (raises)
         q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("%s: q_out without q" % name)
@@ -486,7 +495,7 @@ def bsfa_cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
             raise TypeError("%s: cos_sin must be contiguous float32 [positions, rot_dim]" % name)
         (positions, rot), cs_ptr = cos_sin.shape, cos_sin.data_ptr()
     table, table_stride, pages = _pages("block_table", block_table, B)
-    p = _PACK_APPEND(B, Hq, N, *qs, *_strides("k", k, shape), *_strides("v", v, shape), *qos, *kos,
+    p = _PACK_APPEND(B, Hq, N, *qs[:3], *ks[:3], *vs[:3], *qos[:3], *kos,
                      0 if seqlens is None else _lens("seqlens", seqlens, B), _lens("start", start, B), table, table_stride, pages,
                      cs_ptr, positions, rot, 1 if interleaved else 0)
     device = k.device
@@ -523,7 +532,10 @@ def _attend(call, name, q, k_cache, v_cache, prefix_table, prefix_len, block_tab
         pages_p = prefix_table.numel()
         prefix = _lens("prefix_table", prefix_table, pages_p)
     table, table_stride, pages = _pages("block_table", block_table, B)
-    members = (B, Hq, N, *_strides("q", q, shape), *_strides("out", out, shape), 0 if q_lens is None else _lens("q_lens", q_lens, B),
+    qs, os_ = q.stride(), out.stride()
+    if out.shape != shape or qs[3] != 1 or os_[3] != 1:
+        _strides("q", q, shape), _strides("out", out, shape)                             # (raises)
+    members = (B, Hq, N, *qs[:3], *os_[:3], 0 if q_lens is None else _lens("q_lens", q_lens, B),
                _lens("cache_lens", cache_lens, B), table, table_stride, pages, max_cache_len, prefix, prefix_len, pages_p)
     ws_ptr = ws_bytes = 0
     if workspace is True or call is None:
