@@ -106,7 +106,9 @@ def test_a_batch_dealt_to_the_chip(name, s, hq, hkv, d):
     """Sequences of different lengths share workgroups, and workgroups share sequences: 3 x 8 and 5 x 8 and 9 x 8 rows to a KV head
     take the streaming kernel's wide form and the kernel of many rows."""
     lens = _dealt(name)
-    run_case(lens, s, hq, hkv, d, 16, "bf16" if d == 128 else "fp16", columns=max(17, -(-max(lens) // 16)))
+    columns = max(17, -(-max(lens) // 16))
+    run_case(lens, s, hq, hkv, d, 16, "bf16" if d == 128 else "fp16", columns=columns)
+    run_case(lens, s, hq, hkv, d, 32, q_lens=[(b + s) % (s + 1) for b in range(len(lens))], columns=columns)
 
 
 def test_many_sequences_one_range_each():
@@ -144,6 +146,41 @@ def test_pages_that_the_cache_does_not_have(s):
     paged.check_attention(out.cpu(), lse.cpu(), ref, dt, 7.0)
 
 
+@pytest.mark.parametrize("b,s", [(2, 1), (6, 1), (20, 1), (3, 12)])
+def test_pages_of_the_prefix_that_the_cache_does_not_have(b, s):
+    dt = torch.bfloat16
+    lens = [(40 * x) % 100 for x in range(b)]
+    for prefix, holes in ((600, [0, 7, 37]), (600, range(38)), (16, [0])):
+        kc, vc, table, prefix_table = paged.filled(lens, 16, 2, 128, dt, "nhd", 9, prefix=prefix)
+        for x in holes:
+            prefix_table[x] = -1 if x % 2 else kc.shape[0] + x
+        q = torch.randn(b, s, 8, 128, generator=torch.Generator().manual_seed(5)).to(dt)
+        ref = paged.run_oracle(q, kc, vc, table, lens, prefix_table=prefix_table, prefix_len=prefix)
+        out, lse = torch.full(q.shape, 7.0, dtype=dt, device=DEV), torch.full(q.shape[:3], 7.0, device=DEV)
+        binding.bsfa_prefix_attention(q.to(DEV), kc.to(DEV), vc.to(DEV), prefix_table.to(DEV), prefix, table.to(DEV),
+                                      torch.tensor(lens, dtype=torch.int32, device=DEV), out=out, lse=lse)
+        paged.check_attention(out.cpu(), lse.cpu(), ref, dt, 7.0)
+
+
+@pytest.mark.parametrize("s", [1, 5, 70])
+def test_views(s):
+    """Queries out of a fused projection, results heads first, a table that is a slice of a wider one: nothing beside the
+    results is written."""
+    dt, lens = torch.float16, [300, 9, 77]
+    kc, vc, table, _ = paged.filled(lens, 16, 2, 64, dt, "nhd", 2)
+    g = torch.Generator().manual_seed(5)
+    fused = torch.randn(3, s, 12, 64, generator=g).to(dt)
+    ref = paged.run_oracle(fused[:, :, 2:10], kc, vc, table, lens)
+    wide = torch.full((3, table.shape[1] + 5), 3, dtype=torch.int32)
+    wide[:, 2:-3] = table
+    room = torch.full((3, 10, s + 2, 72), 7.0, dtype=dt, device=DEV)
+    out = room[:, 1:9, 1:-1, :64].transpose(1, 2)
+    binding.bsfa_paged_attention(fused.to(DEV)[:, :, 2:10], kc.to(DEV), vc.to(DEV), wide.to(DEV)[:, 2:-3], torch.tensor(lens, dtype=torch.int32, device=DEV), out=out)
+    paged.check_attention(out.cpu().contiguous(), None, ref, dt, 7.0)
+    out.fill_(7.0)
+    assert (room == 7.0).all()
+
+
 @pytest.mark.parametrize("b,s,hq,hkv", [(1, 1, 4, 2), (5, 1, 8, 2), (9, 2, 12, 4), (20, 1, 4, 1), (40, 1, 8, 2), (70, 3, 3, 1)])
 @pytest.mark.parametrize("prefix", [1, 63, 64, 200, 1000, 2500])
 def test_shared_prefix(b, s, hq, hkv, prefix):
@@ -162,16 +199,32 @@ def test_flat_and_peaked_scores(scale):
     run_case([900, 77], 2, 8, 2, 128, 64, spread_q=scale)
 
 
-def test_offsets_beyond_32_bits():
-    """A cache whose last pages lie more than 2^32 bytes behind its first."""
+@pytest.mark.parametrize("layout", ["nhd", "hnd"])
+def test_offsets_beyond_32_bits(layout):
+    """A cache whose last pages lie more than 2^32 bytes behind its first: appended to, and read by every kernel."""
     dt, page, hkv, d = torch.bfloat16, 64, 2, 128
     n = (1 << 32) // (page * hkv * d * 2) + 40
-    kc, vc = (torch.empty(n, page, hkv, d, dtype=dt, device=DEV) for _ in "kv")
+    shape = (n, page, hkv, d) if layout == "nhd" else (n, hkv, page, d)
+    kc, vc = (torch.empty(shape, dtype=dt, device=DEV) for _ in "kv")
+    if layout == "hnd":
+        kc, vc = kc.transpose(1, 2), vc.transpose(1, 2)
     small_k, small_v, table, _ = paged.filled([300, 65], page, hkv, d, dt, "nhd", 4)
     m = small_k.shape[0]
-    kc[n - m:], vc[n - m:] = small_k.to(DEV), small_v.to(DEV)
-    q = torch.randn(2, 2, 4, d, generator=torch.Generator().manual_seed(5)).to(dt)
-    ref = paged.run_oracle(q, small_k, small_v, table, [300, 65])
-    moved = torch.where((table >= 0) & (table < m), table + (n - m), table)
-    got = binding.bsfa_paged_attention(q.to(DEV), kc, vc, moved.to(DEV), torch.tensor([300, 65], dtype=torch.int32, device=DEV))
-    paged.check_attention(got.cpu(), None, ref, dt, 0.0)
+    moved = torch.where((table >= 0) & (table < m), table + (n - m), table).to(DEV)
+    for b, lens in enumerate((300, 65)):                     # (through the operator that writes it)
+        t = torch.arange(lens)
+        ids = table[b].long()[t // page]
+        rows = [x[ids, t % page][None].to(DEV) for x in (small_k, small_v)]
+        binding.bsfa_cache_append(None, *rows, kc, vc, moved[b:b + 1], torch.zeros(1, dtype=torch.int32, device=DEV))
+        for x, y in ((kc, small_k), (vc, small_v)):
+            assert torch.equal(x[ids.to(DEV) + (n - m), t.to(DEV) % page].cpu(), y[ids, t % page])
+    lens = torch.tensor([300, 65], dtype=torch.int32, device=DEV)
+    for s in (2, 50):
+        q = torch.randn(2, s, 4, d, generator=torch.Generator().manual_seed(5)).to(dt)
+        ref = paged.run_oracle(q, small_k, small_v, table, [300, 65])
+        got = binding.bsfa_paged_attention(q.to(DEV), kc, vc, moved, lens)
+        paged.check_attention(got.cpu(), None, ref, dt, 0.0)
+        none = torch.zeros(2, dtype=torch.int32, device=DEV)
+        got = binding.bsfa_prefix_attention(q.to(DEV), kc, vc, moved[0, :5].contiguous(), 300, moved, none)
+        ref = paged.run_oracle(q, small_k, small_v, table, [0, 0], prefix_table=table[0, :5], prefix_len=300)
+        paged.check_attention(got.cpu(), None, ref, dt, 0.0)
