@@ -547,6 +547,8 @@ def _attend(call, name, q, k_cache, v_cache, prefix_table, prefix_len, block_tab
             ws_ptr = workspace.data_ptr()
     elif workspace is not None and workspace is not False:
         _same_device(name, q, workspace)
+        if not workspace.is_contiguous():
+            raise TypeError("%s: workspace must be contiguous" % name)
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     device = q.device
     _on_device(device, stream, call, c, _PACK_PAGED(*members, ws_ptr, ws_bytes), q.data_ptr(), 1 if causal else 0, out.data_ptr(), lse_ptr)

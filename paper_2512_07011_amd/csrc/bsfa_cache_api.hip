@@ -17,18 +17,19 @@ constexpr int64_t kMaxPlaces = 1 << 30;                 // of one block table
 constexpr int64_t kMaxTokens = 1 << 25, kMaxRows = 1 << 26, kMaxUnits = 1 << 23;      // (grids of less than 2^32 threads)
 constexpr int64_t kMaxTokenStride = 1 << 25;            // a copy addresses 16 tokens of a page with 32-bit offsets
 
-// strides of a tensor's dimensions that have more than one element (those of the others are never used)
-bsfa_status check_strides(const char *name, const int64_t *stride, const int64_t *size, int n, int64_t row)
+// strides of a tensor's dimensions that have more than one element (those of the others are never used); of one that is
+// written no two elements may be the same
+bsfa_status check_strides(const char *name, const int64_t *stride, const int64_t *size, int n, int64_t row, bool written = false)
 {
     for (int x = 0; x < n; ++x) {
         if (size[x] < 2) continue;
         if (stride[x] < 0 || stride[x] % 8) FAIL(BSFA_ERR_SHAPE, "%s: stride #%d = %lld must be a non-negative multiple of 8 elements", name, x, (long long)stride[x]);
-        if (x > 0 && stride[x] < row) FAIL(BSFA_ERR_SHAPE, "%s: stride #%d = %lld is smaller than head_dim", name, x, (long long)stride[x]);
+        if ((x > 0 || written) && stride[x] < row) FAIL(BSFA_ERR_SHAPE, "%s: stride #%d = %lld is smaller than head_dim", name, x, (long long)stride[x]);
     }
     return BSFA_OK;
 }
 
-bsfa_status check_cache(const bsfa_cache *c)
+bsfa_status check_cache(const bsfa_cache *c, bool written = false)
 {
     if (!c) FAIL(BSFA_ERR_NULL, "cache descriptor is NULL");
     if (c->dtype != BSFA_BF16 && c->dtype != BSFA_FP16) FAIL(BSFA_ERR_DTYPE, "dtype %d not supported (bf16 and fp16 only)", c->dtype);
@@ -38,8 +39,8 @@ bsfa_status check_cache(const bsfa_cache *c)
     if (c->head_dim != 64 && c->head_dim != 128) FAIL(BSFA_ERR_UNSUPPORTED, "head_dim %d is not built (64 and 128 are)", c->head_dim);
     const int64_t size[3] = {c->n_pages, c->page_size, c->n_kv_heads};
     const int64_t k[3] = {c->k_stride_page, c->k_stride_n, c->k_stride_h}, v[3] = {c->v_stride_page, c->v_stride_n, c->v_stride_h};
-    bsfa_status s = check_strides("k cache", k, size, 3, c->head_dim);
-    if (s == BSFA_OK) s = check_strides("v cache", v, size, 3, c->head_dim);
+    bsfa_status s = check_strides("k cache", k, size, 3, c->head_dim, written);
+    if (s == BSFA_OK) s = check_strides("v cache", v, size, 3, c->head_dim, written);
     if (s != BSFA_OK) return s;
     if (k[1] > kMaxTokenStride || v[1] > kMaxTokenStride) FAIL(BSFA_ERR_SHAPE, "token strides of the cache must not exceed 2^25 elements");
     return BSFA_OK;
@@ -82,7 +83,7 @@ bsfa_status check_paged(const bsfa_cache *c, const bsfa_paged *p, bool prefix)
     const int64_t size[3] = {p->batch, p->seqlen, p->n_q_heads};
     const int64_t q[3] = {p->q_stride_b, p->q_stride_n, p->q_stride_h}, o[3] = {p->o_stride_b, p->o_stride_n, p->o_stride_h};
     if (s == BSFA_OK) s = check_strides("q", q, size, 3, c->head_dim);
-    if (s == BSFA_OK) s = check_strides("out", o, size, 3, c->head_dim);
+    if (s == BSFA_OK) s = check_strides("out", o, size, 3, c->head_dim, true);
     if (s != BSFA_OK) return s;
     if (prefix && (p->prefix_len < 1 || p->prefix_len > (int64_t)p->prefix_pages * c->page_size))
         FAIL(BSFA_ERR_SHAPE, "prefix_len %d must be positive and fit %d pages of %d tokens", p->prefix_len, p->prefix_pages, c->page_size);
@@ -149,7 +150,7 @@ extern "C" {
 bsfa_status bsfa_cache_append(const bsfa_cache *c, const bsfa_append *p, const void *q, const void *k, const void *v,
                               void *q_out, void *k_out, void *hip_stream)
 {
-    bsfa_status s = check_cache(c);
+    bsfa_status s = check_cache(c, true);
     if (s != BSFA_OK) return s;
     if (!p) FAIL(BSFA_ERR_NULL, "problem descriptor is NULL");
     s = check_batch(c, p->batch, p->n_q_heads, p->seqlen);
@@ -165,7 +166,7 @@ bsfa_status bsfa_cache_append(const bsfa_cache *c, const bsfa_append *p, const v
         {"k_out", k_out, size, {p->ko_stride_b, p->ko_stride_n, p->ko_stride_h}}};
     for (const auto &x : t) {
         if (!x.at) continue;
-        s = check_strides(x.name, x.stride, x.size, 3, c->head_dim);
+        s = check_strides(x.name, x.stride, x.size, 3, c->head_dim, x.at == q_out || x.at == k_out);
         if (s != BSFA_OK) return s;
         if (misaligned(x.at, 16)) FAIL(BSFA_ERR_SHAPE, "%s must be 16-byte aligned", x.name);
     }

@@ -11,7 +11,7 @@
 // operations): memory.  64 sequences of 1K to 8K tokens, 905 MB: 163 us, 5.6 TB/s; two of 128K, 1.07 GB: 185 us, 5.8 TB/s (a
 // large copy moves 4.9 TB/s on the same card, read and written bytes together).  Many rows (a chunk of a prompt, a batch behind one
 // prefix): the matrix pipe and the exponentials beside it.  2048 tokens behind 30K of 32 heads: 965 to 1000 us, 1.07 to 1.11
-// PFLOP/s, the pipe busy in 53 % of the cycles at 1.8 GHz (a large library product reaches 1.32 PFLOP/s).  Small calls: their chain of dependent trips to memory --
+// PFLOP/s, the pipe busy in 67 % of the cycles at 1.56 GHz (a large library product reaches 1.32 PFLOP/s).  Small calls: their chain of dependent trips to memory --
 // lengths, page, keys, the ranges' results -- 9 us for a thousand tokens.
 #include "bsfa_dev.h"
 

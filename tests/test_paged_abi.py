@@ -118,6 +118,28 @@ def test_pointers(lib):
     assert lib.bsfa_paged_attention(c, p, FAKE, 1, FAKE, ctypes.c_void_p(0x10002), None) == -2
 
 
+def test_what_is_written_has_no_two_elements_in_one_place(lib):
+    """A batch of one read tensor is fine (the check behind it answers), one of a written tensor is not."""
+    c, still = ctypes.byref(cache()), dict(workspace=None, prefix_table=0x10000, prefix_len=20, prefix_pages=2)
+    assert lib.bsfa_prefix_attention(c, ctypes.byref(paged(q_stride_b=0, **still)), FAKE, 1, FAKE, None, None) == -5
+    assert lib.bsfa_prefix_attention(ctypes.byref(cache(k_stride_page=0)), ctypes.byref(paged(**still)), FAKE, 1, FAKE, None, None) == -5
+    assert lib.bsfa_prefix_attention(c, ctypes.byref(paged(o_stride_b=0, **still)), FAKE, 1, FAKE, None, None) == -2
+    for kw in (dict(qo_stride_b=0), dict(ko_stride_b=64)):
+        assert lib.bsfa_cache_append(c, ctypes.byref(append(**kw)), FAKE, FAKE, FAKE, ctypes.c_void_p(0x20000), ctypes.c_void_p(0x30000), None) == -2
+        assert b"_out" in lib.bsfa_last_error()
+    for kw in (dict(k_stride_page=0), dict(v_stride_page=0)):
+        assert lib.bsfa_cache_append(ctypes.byref(cache(**kw)), ctypes.byref(append()), FAKE, FAKE, FAKE, FAKE, None, None) == -2
+
+
+def test_workspaces_of_the_binding_are_contiguous(monkeypatch):
+    monkeypatch.setattr(binding, "_same_device", lambda *a: None)
+    monkeypatch.setattr(binding, "_on_device", lambda *a: pytest.fail("launched"))
+    q, kc = torch.zeros(2, 3, 4, 128, dtype=torch.bfloat16), torch.zeros(4, 16, 2, 128, dtype=torch.bfloat16)
+    i, t = torch.zeros(2, dtype=torch.int32), torch.zeros(2, 100, dtype=torch.int32)
+    with pytest.raises(TypeError):
+        binding.bsfa_paged_attention(q, kc, kc, t, i, workspace=torch.zeros(1, dtype=torch.uint8).expand(1 << 24))
+
+
 def test_workspace_follows_the_work(lib):
     """None where sequences are short by the host's knowledge; never more than a fixed number of ranges on top of the batch."""
     c = cache(n_pages=1 << 20)
