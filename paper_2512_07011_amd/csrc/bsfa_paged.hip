@@ -37,7 +37,7 @@ struct Launch {
     PagedParams p;
     // The sequences' own tokens: a unit of `rows` rows each, `groups` workgroups side by side.  shares > 0: the batch's tokens
     // are dealt to so many workgroups evenly (even_share), min_share sub-blocks or more each; 0: one to a sequence.
-    int rows, groups, shares, min_share, near;
+    int rows, groups, shares, min_share, near, range_cost;
     // The prefix: one unit of prefix_rows rows, ranges of prefix_chunk keys.
     int prefix_rows, prefix_groups, prefix_parts, prefix_chunk;
     // Unscaled results of ranges [slot][hkv][rows][d] and their (m, l); slots: see Range, and the prefix's ranges.
@@ -75,8 +75,8 @@ struct Range {
 
 __device__ __forceinline__ int length_of(Params &p, int b) { return min(max(p.cache_lens[b], 0), p.max_len); }
 __device__ __forceinline__ int queries_of(Params &p, int b) { return p.q_lens ? min(max(p.q_lens[b], 0), p.seqlen) : p.seqlen; }
-// sub-blocks of a sequence; an empty one counts as one, so that somebody writes its result
-__device__ __forceinline__ int units_of(int len) { return max(1, (len + kSub - 1) / kSub); }
+// What a sequence counts as, in sub-blocks: its own and what a range's beginning and end take, at least a workgroup's share
+__device__ __forceinline__ int units_of(Args &a, int len) { return max((int)((unsigned)(len + kSub - 1) / kSub) + a.range_cost, a.min_share); }
 
 // The batch's sub-blocks in a row, dealt to `shares` workgroups evenly: workgroup x has those from x * share on, which may
 // begin and end inside sequences.  A border between two workgroups that lies no more than `near` sub-blocks from a border
@@ -118,7 +118,7 @@ __device__ __forceinline__ bool even_share(Args &a, int x, Share &y)
     Params &p = a.p;
     const int lane = threadIdx.x & 63;
     // sub-blocks of sequences b0 .. b0 + lane; all 64 of them
-    auto scan = [&](int b0, int lens) { return scan_lanes(b0 + lane < p.batch ? units_of(lens) : 0); };
+    auto scan = [&](int b0, int lens) { return scan_lanes(b0 + lane < p.batch ? units_of(a, lens) : 0); };
     auto last = [](int upto) { return __builtin_amdgcn_readlane(upto, 63); };
     y.b0 = 0;
     load_lengths(p, 0, y.lens, y.news);
@@ -129,14 +129,14 @@ __device__ __forceinline__ bool even_share(Args &a, int x, Share &y)
         total += last(scan(b0, lens));
     }
     y.share = max((total + a.shares - 1) / a.shares, a.min_share);
-    y.near = min(a.near, y.share / 4);
+    y.near = max(min(a.near, y.share / 4), a.range_cost);
     int before = 0;
     while (true) {
         const int sum = last(upto);
         if ((int64_t)x * y.share < before + sum) {
             const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > x * y.share));
             take_sequence(p, y.b0 + l, y);
-            y.before = before + __builtin_amdgcn_readlane(upto, l) - units_of(y.len);
+            y.before = before + __builtin_amdgcn_readlane(upto, l) - units_of(a, y.len);
             return true;
         }
         before += sum;
@@ -168,7 +168,7 @@ template <bool KEEP, class F> __device__ __forceinline__ void own_ranges(int hk,
     while (true) {
         Args &a = arguments();
         Range r;
-        const int end = y.before + units_of(y.len);
+        const int end = y.before + units_of(a, y.len);
         // borders moved to this sequence's: where it begins or ends close to them
         int lo = from, hi = to;
         if (a.shares) {
@@ -180,7 +180,7 @@ template <bool KEEP, class F> __device__ __forceinline__ void own_ranges(int hk,
         r.len = y.len;
         r.new_tokens = y.new_tokens;
         r.k0 = max(lo - y.before, 0) * kSub;
-        r.k1 = end <= hi ? r.len : (hi - y.before) * kSub;
+        r.k1 = end <= hi ? r.len : min((hi - y.before) * kSub, r.len);
         r.slot = a.shares ? x + y.b : x;
         r.whole = lo <= y.before && end <= hi;
         // where the join finds the sequence's ranges: the borders behind this one that lie inside it begin one each
@@ -980,6 +980,11 @@ static int64_t plan(Launch &a, int head_dim)
     a.min_share = few ? 4 : 16;
     a.near = 8;
     a.shares = p.max_len > 256 && items < (few ? 4 : 2) * kCus ? (int)std::max<int64_t>(1, (few ? 1 : 2) * kCus / side) : 0;
+    // A sequence counts as two sub-blocks more than it has, which is what a range's beginning and end take (not / so, us: 16 sequences of
+    // 20 to 300 tokens 12.0 / 9.8, 13 of 40 to 350 and two KV heads 10.8 / 9.0, 8 short ones behind 2000 tokens 14.7 / 12.4, 44 of 120 to 640, seven
+    // new tokens, 20.1 / 19.0; but 16 of 500, an even number of tiles each, 12.5 / 12.9); few long ones are dealt as they are (two of 32K, 8 new
+    // tokens, 50 / 53).
+    a.range_cost = 4 * p.batch >= a.shares || p.batch * (int64_t)p.max_len <= (int64_t)a.shares * 16 * kSub ? 2 : 0;
     a.own_slots = a.shares + p.batch;
     if (p.prefix) {
         a.prefix_rows = p.batch * a.rows;
