@@ -977,7 +977,10 @@ static int64_t plan(Launch &a, int head_dim)
     // fill the chip four times over (twice) anyway, whose results need no joining (dealt / not, us: 64 sequences of 1K to 8K tokens, 512
     // places, 162 / 183, of 2K each 98 / 95; 96 of 300 to 6000, 768, 140 / 155; 128 of 300 to 1500, 1024, 82 / 79; two workgroups of the
     // streaming kernel to a CU: 64 of 1K to 8K 166, two of 128K 188 instead of 185).
-    a.min_share = few ? 4 : 16;
+    // The least a workgroup gets: a tile to a wave (4 / 8 sub-blocks, us: 16 sequences of 20 to 300 tokens 9.8 / 12.4), six tiles of the kernel of
+    // many rows (16 / 24 / 32, us: 64 new tokens of 12 sequences of 134 to 300 23.3 / 17.4 / 17.5, up to 165 of 5 of 250 to 1800 28.0 / 23.9 / 26.4,
+    // 32 of 4 of 500 to 2000 30.0 / 28.0 / 29.5, a prompt of 1000 23.4 / 24.4 / 25.2).
+    a.min_share = few ? 4 : 24;
     a.near = 8;
     a.shares = p.max_len > 256 && items < (few ? 4 : 2) * kCus ? (int)std::max<int64_t>(1, (few ? 1 : 2) * kCus / side) : 0;
     // A sequence counts as two sub-blocks more than it has, which is what a range's beginning and end take (not / so, us: 16 sequences of
