@@ -1000,7 +1000,9 @@ static int64_t plan(Launch &a, int head_dim)
         // 256 behind 16K 99 / 113, 128 behind 32K 93 / 90; 4 tokens each of 64 behind 32K 165 / 144, two of 256 behind 16K 180 / 173).
         const bool long_products = units * p.prefix > (int64_t)96 * kTileKeys * kCus;
         const int64_t want = std::max<int64_t>(1, (long_products ? 2 : 1) * kCus / units);
-        a.prefix_chunk = std::max(128, (int)((p.prefix + want - 1) / want + 63) / 64 * 64);
+        // (at least 64 / 128 / 192 / 256 tokens, us: 62 sequences of 2 tokens behind 1000 22.2 / 22.0 / 19.6 / 21.2, 27 behind 1900 21.3 / 19.5 / 18.5 / 18.7,
+        // 98 of width 64 behind 1000 21.8 / 21.6 / 19.9 / 20.4, 2 behind 700 8.1 / 7.9 / 8.4 / 8.9)
+        a.prefix_chunk = std::max(192, (int)((p.prefix + want - 1) / want + 63) / 64 * 64);
         a.prefix_parts = (p.prefix + a.prefix_chunk - 1) / a.prefix_chunk;
     }
     const bool joined = a.shares || p.prefix;
