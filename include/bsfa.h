@@ -300,6 +300,7 @@ typedef struct {
  * units.  Query head h reads KV head h / (n_q_heads / n_kv_heads).  Scores, softmax and accumulators are fp32, the
  * probabilities are rounded to the element type for the second product.  Keys and values of places that some row of the
  * element sees must be finite; what else lies in the pages has no influence, NaN included.
+ * A query that is not finite makes its own row NaN, lse included (0 and -INFINITY where every score is -infinite), and no other.
  */
 bsfa_status bsfa_paged_attention(const bsfa_cache *c, const bsfa_paged *p, const void *q, int causal, void *out, float *lse,
                                  void *hip_stream);

@@ -289,8 +289,10 @@ template <bool PREFIX> __device__ __forceinline__ Row row_of(int rows, int group
     return x;
 }
 
-// A row's result: the sum of its weights l and their maximum's exponent m give the log-sum-exp.
-__device__ __forceinline__ float natural_lse(float m, float l) { return l > 0.f ? 0.6931471805599453f * (m + __builtin_amdgcn_logf(l)) : -INFINITY; }
+// A row's result: the sum of its weights l and their maximum's exponent m give the log-sum-exp.  Only l = 0 is a row that sees
+// nothing: a query that is not finite makes l NaN, and both have to show it.
+__device__ __forceinline__ float natural_lse(float m, float l) { return l == 0.f ? -INFINITY : 0.6931471805599453f * (m + __builtin_amdgcn_logf(l)); }
+__device__ __forceinline__ float normaliser(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 // ---- few rows: keys streamed once ---------------------------------------------------------------------
 // A workgroup is four waves on 16 * NRT rows of one unit and one range of keys.  Every wave takes tiles of 16 keys of its own
@@ -505,7 +507,7 @@ __device__ __forceinline__ void stream_range(Args &a, const Range r, int hk, int
         if (!y.stored) continue;
         if (direct) {
             if (y.i >= qn) continue;
-            const float f = ll > 0.f ? 1.f / ll : 0.f;   // (a row that sees nothing: 0)
+            const float f = normaliser(ll);
             uint16_t *dst = z.p.out + y.b * z.p.osb + y.i * z.p.osn + y.h * z.p.osh + jd;
             typedef el elx __attribute__((ext_vector_type(DPT)));
             elx w;
@@ -794,7 +796,7 @@ __device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int r
     l += __shfl_xor(l, 32);
     Args &z = arguments();
     const int end_rows = PREFIX ? z.prefix_rows : z.rows;
-    const float f = !direct ? 1.f : l > 0.f ? 1.f / l : 0.f;
+    const float f = direct ? normaliser(l) : 1.f;
     constexpr int CH = D / 4;                            // 16-byte chunks of a row of 32-bit results
     float *const ro = reinterpret_cast<float *>(shared.ring) + wave * 32 * D;
 #pragma unroll
@@ -952,7 +954,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const Launch)
             for (int e = 0; e < 4; ++e) o[e] = fmaf(red_o[y][at_lane][e], w, o[e]);
         }
     }
-    const float f = l > 0.f ? 1.f / l : 0.f;
+    const float f = normaliser(l);
     *reinterpret_cast<el4 *>(p.out + b * p.osb + i * p.osn + h * p.osh + at_lane * 4) = el4{(el)(o[0] * f), (el)(o[1] * f), (el)(o[2] * f), (el)(o[3] * f)};
     if (p.lse && at_lane == 0) p.lse[((int64_t)b * p.seqlen + i) * p.hq + h] = natural_lse(m, l);
 }
