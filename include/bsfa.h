@@ -231,7 +231,10 @@ size_t bsfa_calibrate_workspace_bytes(const bsfa_problem *p);
  * batch element lies in page block_table[t / page_size] of the element's row, at place t % page_size.  Page ids
  * outside [0, n_pages) hold nothing: appending drops what would go there, attention does not see it.
  * The three entry points enqueue kernels only: no allocation, no copy, no host synchronisation.  They may be
- * captured into a graph; lengths, positions and tables are read when the graph runs. */
+ * captured into a graph; lengths, positions and tables are read when the graph runs.
+ * Of a tensor that a call writes (out, q_out, k_out, the cache that is appended to) no two elements may lie in one place:
+ * each stride is as large as all that the dimensions of smaller strides hold, else BSFA_ERR_SHAPE.  Tensors that are only
+ * read may repeat (a stride of 0 over the batch, or over the pages of the cache). */
 typedef struct {
     int32_t n_pages, page_size;   /* page_size: a power of two, at least 16 */
     int32_t n_kv_heads, head_dim; /* head_dim 64 or 128 */

@@ -17,14 +17,25 @@ constexpr int64_t kMaxPlaces = 1 << 30;                 // of one block table
 constexpr int64_t kMaxTokens = 1 << 25, kMaxRows = 1 << 26, kMaxUnits = 1 << 23;      // (grids of less than 2^32 threads)
 constexpr int64_t kMaxTokenStride = 1 << 25;            // a copy addresses 16 tokens of a page with 32-bit offsets
 
-// strides of a tensor's dimensions that have more than one element (those of the others are never used); of one that is
-// written no two elements may be the same
+// strides of a tensor's dimensions that have more than one element (those of the others are never used).  Of a tensor that is
+// written no two elements may be the same: a dimension's step lies behind all that the dimensions of smaller steps hold.
 bsfa_status check_strides(const char *name, const int64_t *stride, const int64_t *size, int n, int64_t row, bool written = false)
 {
+    int order[3], dims = 0;                              // by step, the smallest first
     for (int x = 0; x < n; ++x) {
         if (size[x] < 2) continue;
         if (stride[x] < 0 || stride[x] % 8) FAIL(BSFA_ERR_SHAPE, "%s: stride #%d = %lld must be a non-negative multiple of 8 elements", name, x, (long long)stride[x]);
         if ((x > 0 || written) && stride[x] < row) FAIL(BSFA_ERR_SHAPE, "%s: stride #%d = %lld is smaller than head_dim", name, x, (long long)stride[x]);
+        int y = dims++;
+        for (; y > 0 && stride[order[y - 1]] > stride[x]; --y) order[y] = order[y - 1];
+        order[y] = x;
+    }
+    int64_t held = row;
+    for (int y = 0; written && y < dims; ++y) {
+        const int64_t step = stride[order[y]];
+        if (step < held) FAIL(BSFA_ERR_SHAPE, "%s: stride #%d = %lld: two elements would be written to one place", name, order[y], (long long)step);
+        if (step > INT64_MAX / size[order[y]]) FAIL(BSFA_ERR_SHAPE, "%s: stride #%d = %lld exceeds the address space", name, order[y], (long long)step);
+        held += (size[order[y]] - 1) * step;
     }
     return BSFA_OK;
 }
