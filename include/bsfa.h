@@ -269,7 +269,7 @@ typedef struct {
  * Rotates the new tokens' keys by their positions, writes keys and values into the cache, and writes the rotated
  * queries to q_out and, if k_out is not NULL, the rotated keys there as well (what bsfa_forward takes for a prompt):
  *   (a, b) -> (a cos - b sin, b cos + a sin) for every pair, in 32 bits, rounded once.
- * q_out may be q and k_out may be k.  q NULL: keys and values only.  No two tokens of a call may have the same place.
+ * q_out may be q and k_out may be k, with the same strides.  q NULL: keys and values only.  No two tokens of a call may have the same place.
  */
 bsfa_status bsfa_cache_append(const bsfa_cache *c, const bsfa_append *p, const void *q, const void *k, const void *v,
                               void *q_out, void *k_out, void *hip_stream);

@@ -181,6 +181,13 @@ bsfa_status bsfa_cache_append(const bsfa_cache *c, const bsfa_append *p, const v
         if (s != BSFA_OK) return s;
         if (misaligned(x.at, 16)) FAIL(BSFA_ERR_SHAPE, "%s must be 16-byte aligned", x.name);
     }
+    const int in_place[2][2] = {{0, 1}, {2, 4}};         // q and q_out, k and k_out
+    for (const auto &pair : in_place) {
+        const auto &in = t[pair[0]], &out = t[pair[1]];
+        for (int y = 0; in.at && in.at == out.at && y < 3; ++y)
+            if (in.size[y] > 1 && in.stride[y] != out.stride[y])
+                FAIL(BSFA_ERR_SHAPE, "%s at the place of %s must have its strides (#%d: %lld, %lld)", out.name, in.name, y, (long long)out.stride[y], (long long)in.stride[y]);
+    }
     if (misaligned(c->k, 16) || misaligned(c->v, 16)) FAIL(BSFA_ERR_SHAPE, "the cache must be 16-byte aligned");
     if (misaligned(p->seqlens, 4) || misaligned(p->start, 4)) FAIL(BSFA_ERR_SHAPE, "seqlens and start must be 4-byte aligned");
     if (p->interleaved != 0 && p->interleaved != 1) FAIL(BSFA_ERR_SHAPE, "interleaved must be 0 or 1");

@@ -44,3 +44,17 @@ def test_a_written_cache_has_one_place_for_every_element(lib, side, strides, sha
     code = lib.bsfa_cache_append(ctypes.byref(c), ctypes.byref(append(interleaved=2)), FAKE, FAKE, FAKE, OUT, KOUT, None)
     assert code == -2 and ((side + " cache").encode() in lib.bsfa_last_error()) == shared            # (else what stops it: interleaved)
     assert lib.bsfa_prefix_attention(ctypes.byref(c), ctypes.byref(paged(**STOPS)), FAKE, 1, FAKE, None, None) == -5
+
+
+@pytest.mark.parametrize("t, other", [("q", "qo"), ("k", "ko")])
+def test_in_place_means_the_same_strides(lib, t, other):
+    """A result at its input's address, laid out otherwise, would be written where other tokens are still to be read."""
+    c, here = ctypes.byref(cache()), [FAKE, FAKE, FAKE, OUT, KOUT]
+    here[3 if t == "q" else 4] = FAKE
+    for x, strides in enumerate(((5120, 1024, 256), (2560, 128, 640), (2568, 512, 128))):
+        p = append(interleaved=2, **dict(zip((other + "_stride_b", other + "_stride_n", other + "_stride_h"), strides)))
+        assert lib.bsfa_cache_append(c, ctypes.byref(p), *here, None) == -2 and b"at the place of" in lib.bsfa_last_error()
+        assert lib.bsfa_cache_append(c, ctypes.byref(p), FAKE, FAKE, FAKE, OUT, KOUT, None) == -2 and b"interleaved" in lib.bsfa_last_error()
+    one = append(batch=1, interleaved=2, **{other + "_stride_b": 8})             # (never used: one element)
+    assert lib.bsfa_cache_append(c, ctypes.byref(one), *here, None) == -2 and b"interleaved" in lib.bsfa_last_error()
+    assert lib.bsfa_cache_append(c, ctypes.byref(append(interleaved=2)), *here, None) == -2 and b"interleaved" in lib.bsfa_last_error()
