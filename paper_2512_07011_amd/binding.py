@@ -535,6 +535,8 @@ def _attend(call, name, q, k_cache, v_cache, prefix_table, prefix_len, block_tab
     qs, os_ = q.stride(), out.stride()
     if out.shape != shape or qs[3] != 1 or os_[3] != 1:
         _strides("q", q, shape), _strides("out", out, shape)                             # (raises)
+    if call is None:
+        os_ = (N * Hq * d, Hq * d, d)                        # (`out` stands for a result of q's shape: q itself may repeat)
     members = (B, Hq, N, *qs[:3], *os_[:3], 0 if q_lens is None else _lens("q_lens", q_lens, B),
                _lens("cache_lens", cache_lens, B), table, table_stride, pages, max_cache_len, prefix, prefix_len, pages_p)
     ws_ptr = ws_bytes = 0
