@@ -279,7 +279,8 @@ typedef struct {
     int32_t batch, n_q_heads, seqlen;   /* seqlen: new tokens (rows of q) of each batch element, one or more */
     int64_t q_stride_b, q_stride_n, q_stride_h, o_stride_b, o_stride_n, o_stride_h;
     const int32_t *q_lens;        /* optional, DEVICE [batch]: new tokens of each element, clamped to [0, seqlen]; rows of
-                                     out and lse behind them are left untouched.  NULL: all have seqlen. */
+                                     out and lse behind them are left untouched.  0: the element rests, and nothing of
+                                     its own pages is read.  NULL: all have seqlen. */
     const int32_t *cache_lens;    /* DEVICE [batch]: tokens each element has in its own pages, the new ones included,
                                      clamped to what the block table holds.  May be 0. */
     const int32_t *block_table;   /* DEVICE [batch] rows of table_pages page ids */

@@ -73,8 +73,14 @@ struct Range {
     bool whole;                      // ... unless this is all of the sequence
 };
 
-__device__ __forceinline__ int length_of(Params &p, int b) { return min(max(p.cache_lens[b], 0), p.max_len); }
 __device__ __forceinline__ int queries_of(Params &p, int b) { return p.q_lens ? min(max(p.q_lens[b], 0), p.seqlen) : p.seqlen; }
+// A sequence's tokens and its rows' tokens.  One that rests, with tokens but none to compute, counts as one without: nobody sees them.
+__device__ __forceinline__ void lengths_of(Params &p, int b, int &len, int &news)
+{
+    const int n = p.cache_lens[b];
+    news = queries_of(p, b);
+    len = news ? min(max(n, 0), p.max_len) : 0;
+}
 // What a sequence counts as, in sub-blocks: its own and what a range's beginning and end take, at least a workgroup's share
 __device__ __forceinline__ int units_of(Args &a, int len) { return max((int)((unsigned)(len + kSub - 1) / kSub) + a.range_cost, a.min_share); }
 
@@ -90,9 +96,7 @@ struct Share {
 };
 __device__ __forceinline__ void load_lengths(Params &p, int b0, int &lens, int &news)
 {
-    const int b = min(b0 + (int)(threadIdx.x & 63), p.batch - 1);
-    lens = length_of(p, b);
-    news = queries_of(p, b);
+    lengths_of(p, min(b0 + (int)(threadIdx.x & 63), p.batch - 1), lens, news);
 }
 __device__ __forceinline__ void take_sequence(Params &p, int b, Share &y)
 {
@@ -161,8 +165,9 @@ template <bool KEEP, class F> __device__ __forceinline__ void own_ranges(int hk,
         } else {
             y.b = x;
             y.before = y.b0 = 0;
-            y.len = __builtin_amdgcn_readfirstlane(length_of(a.p, x));
-            y.new_tokens = __builtin_amdgcn_readfirstlane(queries_of(a.p, x));
+            lengths_of(a.p, x, y.len, y.new_tokens);
+            y.len = __builtin_amdgcn_readfirstlane(y.len);
+            y.new_tokens = __builtin_amdgcn_readfirstlane(y.new_tokens);
         }
     }
     while (true) {
@@ -195,8 +200,9 @@ template <bool KEEP, class F> __device__ __forceinline__ void own_ranges(int hk,
         if (!z.shares || end >= to || y.b + 1 >= z.p.batch) return;
         if constexpr (KEEP) take_sequence(z.p, y.b + 1, y);
         else {
-            y.len = __builtin_amdgcn_readfirstlane(length_of(z.p, ++y.b));
-            y.new_tokens = __builtin_amdgcn_readfirstlane(queries_of(z.p, y.b));
+            lengths_of(z.p, ++y.b, y.len, y.new_tokens);
+            y.len = __builtin_amdgcn_readfirstlane(y.len);
+            y.new_tokens = __builtin_amdgcn_readfirstlane(y.new_tokens);
         }
     }
 }
@@ -335,6 +341,7 @@ __device__ __forceinline__ void stream_range(Args &a, const Range r, int hk, int
     const int k0 = r.k0, rows = PREFIX ? a.prefix_rows : a.rows;
     int k1 = r.k1;
     const int row0 = rg * kSub * NRT;
+    if (!PREFIX && row0 >= qn * p.group) return;         // (no row that anybody reads)
     const int n16 = lane & 15, quad = lane >> 4;
     int sees[NRT];                                       // keys below it are visible to this lane's row
     int all_see = k1;                                    // ... to every row
@@ -558,7 +565,7 @@ __device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int r
     int k1 = r.k1;
     const int row0 = rg * kTileRows;
     const bool direct = a.direct && r.whole;
-    if (direct && row0 >= qn * p.group) return;          // (no row to store)
+    if (!PREFIX && row0 >= qn * p.group) return;         // (no row that anybody reads)
     const int l32 = lane & 31, hh = lane >> 5;
     const Row mine = row_of<PREFIX>(rows, p.group, p.seqlen, row0 + wave * 32 + l32, r.b, hk);
     int sees = k1, all_see = k1;
