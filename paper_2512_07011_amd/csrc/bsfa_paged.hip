@@ -31,6 +31,11 @@ constexpr float kNone = -3.0e38f;    // running maximum of a row that has seen n
 // below 2^8, which costs no precision, and accumulators are hardly ever rescaled (with a growth of nothing allowed, some row of
 // 32 grows in one tile of five over 32K keys).
 constexpr float kSlack = 8.f;
+// fp16: what a row's exponent m is kept below its maximum by, so that weights reach 2^15 at most (with kSlack) and only those below
+// 2^-32 of the largest round to 0.  Without it that was 2^-25, and 16384 keys of e^-17.5 of one other's weight each were lost,
+// of e^-16 came out 6 % off.  bf16 has the exponents of 32 bits.  l and the accumulators have the same factor, and (m, l) mean
+// the same wherever ranges are joined.
+template <bool F16> constexpr float kLift = F16 ? 7.f : 0.f;
 constexpr int kSub = 16;             // keys that lie in one page whatever its size
 
 struct Launch {
@@ -444,7 +449,7 @@ __device__ __forceinline__ void stream_range(Args &a, const Range r, int hk, int
         el4 pr[NRT];
 #pragma unroll
         for (int t = 0; t < NRT; ++t) {
-            float mx = quad_max(fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3]))) * p.scale_log2;
+            float mx = quad_max(fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3]))) * p.scale_log2 - kLift<F16>;
             if (__builtin_amdgcn_ballot_w64(mx > m[t] + kSlack)) {
                 mx = mx > m[t] + kSlack ? mx : m[t];
                 const float f = __builtin_amdgcn_exp2f(m[t] - mx);
@@ -650,7 +655,7 @@ __device__ __forceinline__ void tile_range(Args &a, const Range r, int hk, int r
             }
     };
     auto new_max = [&](float mx) {                       // of the raw scores, in both lanes of the row
-        mx *= p.scale_log2;
+        mx = mx * p.scale_log2 - kLift<F16>;
         const float y = mx > m + kSlack ? mx : m;
         grown = __builtin_amdgcn_ballot_w64(y > m);
         alpha = __builtin_amdgcn_exp2f(m - y);
