@@ -1,7 +1,7 @@
 // Attention of new tokens over a paged K/V cache for gfx950, wave64, bf16 or fp16 MFMA:
 //     o_i = sum_t softmax_t(q_i k_t / sqrt(d)) v_t
 // over the tokens t that query i sees: those its sequence has in its own pages (causal: up to i's own place) and those of a
-// prefix that all sequences share.  One pass over the keys with a running maximum m, normaliser l and unscaled accumulator
+// prefix that all sequences share.  One pass over the keys with a running maximum m (fp16: 7 less, kLift), normaliser l and unscaled accumulator
 // O; ranges of keys are worked on apart and joined by
 //     m = max m_x,  l = sum l_x 2^(m_x - m),  O = sum O_x 2^(m_x - m)          (log2 units).
 // The (query token, query head) pairs that read one KV head are the rows of a unit: one sequence's, or for the prefix
@@ -10,8 +10,8 @@
 // What bounds it.  Few rows to a key (decoding: the query heads of a KV head, 512 bytes of K and V for 4 d times as many
 // operations): memory.  64 sequences of 1K to 8K tokens, 905 MB: 163 us, 5.6 TB/s; two of 128K, 1.07 GB: 185 us, 5.8 TB/s (a
 // large copy moves 4.9 TB/s on the same card, read and written bytes together).  Many rows (a chunk of a prompt, a batch behind one
-// prefix): the matrix pipe and the exponentials beside it.  2048 tokens behind 30K of 32 heads: 965 to 1000 us, 1.07 to 1.11
-// PFLOP/s, the pipe busy in 67 % of the cycles at 1.56 GHz (a large library product reaches 1.32 PFLOP/s).  Small calls: their chain of dependent trips to memory --
+// prefix): the matrix pipe and the exponentials beside it.  2048 tokens behind 30K of 32 heads: 965 us, 1.11 PFLOP/s (other cards
+// 925 to 1000 us), the pipe busy in 67 % of the cycles at 1.56 GHz (a large library product reaches 1.32 PFLOP/s).  Small calls: their chain of dependent trips to memory --
 // lengths, page, keys, the ranges' results -- 9 us for a thousand tokens.
 #include "bsfa_dev.h"
 
@@ -973,9 +973,10 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const Launch)
 
 // ---- launch -----------------------------------------------------------------------------------------------
 constexpr int kCus = 256;
-// Up to that many rows of a unit are streamed; three or four 16-row sets of accumulators do not fit the registers of two waves to a
-// SIMD (streamed / with the kernel of many rows, us, 32 rows: 8 sequences of 2K to 8K tokens 37 / 42, two of 32K 51 / 54, 24 of 700 to 6000
-// of width 64 25.5 / 32.4, but 64 of 100 to 500 30 / 25; 16 rows: 16 of 1K to 4K 31 / 39).
+// Up to that many rows of a unit, one or two 16-row sets of accumulators, are streamed (streamed / with the kernel of many rows, us, 32
+// rows: 8 sequences of 2K to 8K tokens 37 / 42, two of 32K 51 / 54, 24 of 700 to 6000 of width 64 25.5 / 32.4, but 64 of 100 to 500 30 / 25;
+// 16 rows: 16 of 1K to 4K 31 / 39).  Three sets, and four at width 64, would fit the registers of two waves to a SIMD (212 and 162 of
+// 256), four at width 128 would not (48 bytes spilled); 33 rows and more have not been measured in this kernel.
 constexpr int kFewRows = 32;
 static int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 static int row_groups(int rows) { return rows <= kFewRows ? 1 : (rows + kTileRows - 1) / kTileRows; }
@@ -1011,7 +1012,8 @@ static int64_t plan(Launch &a, int head_dim)
         const int64_t units = (int64_t)p.hkv * a.prefix_groups;
         // One workgroup of the prefix to a CU leaves the other place to the own tokens, which then arrive while the prefix is
         // multiplied; two multiply faster, which counts where that takes longest (one / two, us: 64 sequences behind 32K 64 / 75,
-        // 256 behind 16K 99 / 113, 128 behind 32K 93 / 90; 4 tokens each of 64 behind 32K 165 / 144, two of 256 behind 16K 180 / 173).
+        // 256 behind 16K 99 / 113; 4 tokens each of 64 behind 32K 165 / 144, two of 256 behind 16K 180 / 173).  The line goes by the products alone:
+        // 128 sequences behind 32K have as many as 256 behind 16K and get one workgroup, too, though two would be faster (93 / 90).
         const bool long_products = units * p.prefix > (int64_t)96 * kTileKeys * kCus;
         const int64_t want = std::max<int64_t>(1, (long_products ? 2 : 1) * kCus / units);
         // (at least 64 / 128 / 192 / 256 tokens, us: 62 sequences of 2 tokens behind 1000 22.2 / 22.0 / 19.6 / 21.2, 27 behind 1900 21.3 / 19.5 / 18.5 / 18.7,
