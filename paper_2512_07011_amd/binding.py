@@ -456,8 +456,8 @@ def bsfa_cache_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tenso
     rotated keys: what bsfa_forward takes for a prompt; else None.  Enqueues on ``stream`` (default: torch's current
     stream)."""
     name = "bsfa_cache_append"
-    if k_out is True:
-        k_out = _empty_like(k, stream)
+    if k_out is True or k_out is False:
+        k_out = _empty_like(k, stream) if k_out else None
     _same_device(name, k, q, v, k_cache, v_cache, block_table, start, cos_sin, seqlens, q_out, k_out)
     c, (_, _, Hkv, d), dtype = _cache(name, k_cache, v_cache)
     shape = k.shape
