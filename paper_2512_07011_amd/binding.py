@@ -398,6 +398,8 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 
 def _on_device(device, stream, call, *args):
     """call(*args, stream) with `device` current: the kernels of a stream are launched from its own device."""
+    if stream is not None and stream.device != device:
+        raise ValueError("bsfa: the stream must be one of the tensors' GPU")
     if device.index == _current_device():
         rc = call(*args, _raw_stream(stream, device))
     else:

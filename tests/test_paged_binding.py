@@ -43,3 +43,14 @@ def test_rotated_keys_are_asked_for_or_not(recorded):
     assert k.shape == a[1].shape and recorded.calls[-1][6] == k.data_ptr()
     q, k = binding.bsfa_cache_append(*a, k_out=a[1])
     assert k is a[1] and recorded.calls[-1][6] == a[1].data_ptr()
+
+
+def test_a_stream_of_another_device_is_refused(monkeypatch):
+    """Kernels on it would run where the tensors are not."""
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    here, there = (types.SimpleNamespace(device=torch.device("cuda", x), cuda_stream=5 + x) for x in (0, 1))
+    launched = []
+    binding._on_device(torch.device("cuda", 0), here, lambda *a: launched.append(a), 1, 2)
+    assert launched == [(1, 2, 5)]
+    with pytest.raises(ValueError):
+        binding._on_device(torch.device("cuda", 0), there, lambda *a: pytest.fail("launched"), 1, 2)
