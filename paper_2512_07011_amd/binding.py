@@ -372,6 +372,8 @@ def alloc_cache(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, dt
 def rotary_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
     """[n_positions, rot_dim] fp32: of every position the cosines of its rot_dim / 2 angles
     position * base ** (-2 i / rot_dim), then their sines.  The angles are taken in 64 bits."""
+    if rot_dim < 2 or rot_dim % 2:
+        raise ValueError("rotary_table: rot_dim must be positive and even, is %d" % rot_dim)
     freq = base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device) / rot_dim)
     angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * freq
     return torch.cat([angle.cos(), angle.sin()], dim=1).float()

@@ -54,3 +54,10 @@ def test_a_stream_of_another_device_is_refused(monkeypatch):
     assert launched == [(1, 2, 5)]
     with pytest.raises(ValueError):
         binding._on_device(torch.device("cuda", 0), there, lambda *a: pytest.fail("launched"), 1, 2)
+
+
+@pytest.mark.parametrize("rot", [0, -2, 1, 15, 63])
+def test_rotation_tables_have_pairs(rot):
+    """An odd width has no pairs: the table came out a column wider, for a rotation of other angles than the width says."""
+    with pytest.raises(ValueError):
+        binding.rotary_table(8, rot, device="cpu")
